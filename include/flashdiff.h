@@ -358,6 +358,144 @@ fd_status fd_beta_flow_cascade(const void* const* Xs, const fd_dtype* xts, const
                                double* evals, float* evecs, float* psi, void* ws, size_t ws_bytes,
                                void* stream);
 
+/* ---- a parametric extension of the coordinates ----
+ *
+ * The coordinates psi are defined on the sampled points; the Nystrom extension
+ * needs all of them for every new point.  A network x -> psi(x) trained on the
+ * eigenvectors takes its place.  Its operators: layer norm, the gated
+ * feed-forward block (first, inner and last layers alike, since its output
+ * width is free), both with their backward passes, and the AdamW step.
+ *
+ *  - All entry points of this section are asynchronous on `stream`, allocate
+ *    nothing and use no atomics: repeated calls give identical bits.
+ *  - Matrices are row-major with a leading dimension of their own; any sizes,
+ *    leading dimensions and element-aligned pointers are taken.  16-byte
+ *    aligned pointers with leading dimensions and widths that are multiples of
+ *    16 bytes are the fast case.  N = 0 rows are allowed: nothing is written but the
+ *    gradients of weights and biases, which are then zero.
+ *  - FD_F32 computes to float32 accuracy; FD_BF16 accumulates in float32 and
+ *    rounds each stored value once.
+ *  - Non-finite inputs are not refused: they come out as NaN or infinity where the
+ *    formulas let them through, and rows that do not meet them stay clean. */
+
+/* Layer norm over the D features of each of N rows:
+ *     y = (x - mean) rstd gamma + beta,  rstd = (mean((x - mean)^2) + eps)^-1/2.
+ *   X, Y: N x D (device, dtype xt).  Y may be X with ldy == ldx.
+ *   gamma, beta: D values (device, dtype wt), or NULL for ones / zeros.  eps >= 0.
+ *   stats: N pairs (mean, rstd) of floats (device, 8-byte aligned) for the backward pass, or NULL. */
+fd_status fd_layer_norm(const void* X, fd_dtype xt, int64_t N, int64_t D, int64_t ldx,
+                        const void* gamma, const void* beta, fd_dtype wt, float eps, void* Y,
+                        int64_t ldy, float* stats, void* stream);
+
+/* Bytes of workspace of fd_layer_norm_backward (0 for sizes that it rejects). */
+size_t fd_layer_norm_workspace_size(int64_t N, int64_t D);
+
+/* Backward pass of fd_layer_norm: with g = dy gamma and h = (x - mean) rstd,
+ *     dx = rstd (g - mean(g) - h mean(g h)) [+ add],
+ *     dgamma = sum over rows of dy h,  dbeta = sum over rows of dy.
+ *   dY, X, dX, add: N x D (device, dtype xt); add (NULL: none) is the gradient of a
+ *     residual branch.  dX may be dY or add, with the same leading dimension.
+ *   gamma: as in the forward pass.  stats: what it wrote.
+ *   dgamma, dbeta: D values (device, dtype wt), or NULL. */
+fd_status fd_layer_norm_backward(const void* dY, int64_t lddy, const void* X, fd_dtype xt,
+                                 int64_t N, int64_t D, int64_t ldx, const void* gamma, fd_dtype wt,
+                                 const float* stats, const void* add, int64_t ldadd, void* dX,
+                                 int64_t lddx, void* dgamma, void* dbeta, void* ws,
+                                 size_t ws_bytes, void* stream);
+
+typedef enum fd_activation {
+  FD_ACT_SILU = 0, /* g / (1 + exp(-g)) */
+  FD_ACT_GELU = 1  /* g (1 + erf(g / sqrt 2)) / 2 */
+} fd_activation;
+
+/* Gated feed-forward block D -> F -> O:
+ *     G = X Wg^T + bg,  U = X Wu^T + bu,  H = act(G) * U,  Y = H Wd^T + bd [+ R]. */
+typedef struct fd_gated_block {
+  int64_t N, D, F, O;   /* rows; input, inner and output widths */
+  int32_t type;         /* fd_dtype of X, the weights, the biases, Y and all gradients */
+  int32_t act;          /* fd_activation */
+  const void* X;        /* N x D */
+  const void *Wg, *Wu;  /* F x D each */
+  const void* Wd;       /* O x F */
+  const void *bg, *bu;  /* F values each, or NULL each */
+  const void* bd;       /* O values, or NULL */
+  int64_t ldx, ldwi, ldwd; /* leading dimensions of X, of Wg and Wu, of Wd */
+} fd_gated_block;
+
+/* Where the backward pass writes; NULL = not wanted. */
+typedef struct fd_gated_grads {
+  void* dX;             /* N x D */
+  void *dWg, *dWu;      /* F x D each */
+  void* dWd;            /* O x F */
+  void *dbg, *dbu;      /* F values each */
+  void* dbd;            /* O values */
+  int64_t lddx, lddwi, lddwd;
+} fd_gated_grads;
+
+/* Bytes of the buffer that carries a forward pass's G and U (float32, in the
+ * kernels' own order) to the backward pass. */
+size_t fd_gated_saved_size(const fd_gated_block* b);
+
+/* Bytes of workspace of fd_gated_forward (backward = 0) or fd_gated_backward
+ * (1: with saved, 2: without), whatever the alignments.  0 for sizes that they reject; only
+ * N, D, F, O and type are read. */
+size_t fd_gated_workspace_size(const fd_gated_block* b, int32_t backward);
+
+/* Y (N x O), with R (N x O or NULL) added; Y may be R with the same leading
+ * dimension, and overlaps no other input.  saved: fd_gated_saved_size bytes
+ * (device, 256-byte aligned) that receive G and U, or NULL. */
+fd_status fd_gated_forward(const fd_gated_block* b, const void* R, int64_t ldr, void* Y,
+                           int64_t ldy, void* saved, size_t saved_bytes, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* With dH = dY Wd, dG = dH * U * act'(G), dU = dH * act(G):
+ *     dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X,  dWd = dY^T H,
+ *     dbg, dbu, dbd = column sums of dG, dU, dY.  (The gradient of R is dY.)
+ *   saved: what the forward pass wrote, or NULL to compute G and U again.
+ *   No output may overlap an input. */
+fd_status fd_gated_backward(const fd_gated_block* b, const void* dY, int64_t lddy,
+                            const void* saved, size_t saved_bytes, const fd_gated_grads* grads,
+                            void* ws, size_t ws_bytes, void* stream);
+
+/* One tensor of an AdamW step.  All arrays hold n elements (device, contiguous). */
+typedef struct fd_adamw_tensor {
+  float* p;          /* parameters, float32, updated */
+  const void* g;     /* gradients, of dtype gt */
+  void* m;           /* first moment: float32, or 8-bit e4m3 values */
+  void* v;           /* second moment: float32, or its square root as 8-bit e4m3 values */
+  float* m_scale;    /* 8-bit states: a scale for each 256 elements (the last may be fewer) */
+  float* v_scale;
+  void* copy;        /* bfloat16 copy of the updated parameters, or NULL */
+  int64_t n;         /* >= 0 */
+  int32_t gt;        /* fd_dtype of g */
+  float decay;       /* multiplies the step's weight decay (0: none) */
+} fd_adamw_tensor;
+
+typedef struct fd_adamw_opts {
+  double lr, beta1, beta2, eps, weight_decay; /* defaults 1e-3, 0.9, 0.999, 1e-8, 0.01 */
+  double grad_scale;  /* multiplies every gradient. Default 1 */
+  int64_t step;       /* 1 for the first step: the moments are divided by 1 - beta^step */
+  int32_t state_bits; /* 32 or 8. Default 32 */
+  int32_t reserved;
+} fd_adamw_opts;
+
+/* Fill *opts with the defaults (step = 1). */
+void fd_adamw_default_opts(fd_adamw_opts* opts);
+
+/* One step over `count` tensors (host array):
+ *     m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *     p = p (1 - lr wd) - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps).
+ * 8-bit states hold e4m3 values times a scale, the largest finite magnitude of
+ * each 256 elements / 448: m, and r = sqrt(v), whose positive values never
+ * round to zero.  A step widens them, updates p from the
+ * unrounded moments, and rounds them back (to nearest, ties to even); an
+ * element that is not finite is kept as NaN and leaves its neighbours alone.
+ * Clear m, v and the scales before the first step.
+ * The pointers travel with the launches (the tensors of one call share a few):
+ * the array may go once the call returns. */
+fd_status fd_adamw_step(const fd_adamw_tensor* tensors, int64_t count, const fd_adamw_opts* opts,
+                        void* stream);
+
 /* ---- diagnostics: kernel timing with HIP events ----
  * When enabled, every launch of the fused product kernel (FD_KERNEL_PRODUCT)
  * and of the row-sum kernel of the normalisation passes (FD_KERNEL_ROWSUM) is

@@ -37,8 +37,11 @@ EXPORTS = (
     "fd_block_lanczos", "fd_continuation", "fd_last_error", "fd_status_string",
     "fd_profile_enable", "fd_profile_read", "fd_flow_default_opts", "fd_beta_flow",
     "fd_beta_flow_cascade", "fd_degree_dyadic", "fd_kernel_matmul_noalloc",
-    "fd_kernel_matmul_noalloc_limit",
+    "fd_kernel_matmul_noalloc_limit", "fd_layer_norm", "fd_layer_norm_workspace_size",
+    "fd_layer_norm_backward", "fd_gated_saved_size", "fd_gated_workspace_size",
+    "fd_gated_forward", "fd_gated_backward", "fd_adamw_default_opts", "fd_adamw_step",
 )
+FD_ACT = {"silu": 0, "gelu": 1}
 FD_KERNEL_PRODUCT, FD_KERNEL_ROWSUM = 0, 1
 
 
@@ -84,6 +87,36 @@ class FlowProbe(ctypes.Structure):
 
     def as_dict(self) -> dict:
         return {f: getattr(self, f) for f, _ in self._fields_ if f != "reserved"}
+
+
+class GatedBlock(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("D", ctypes.c_int64), ("F", ctypes.c_int64),
+                ("O", ctypes.c_int64), ("type", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("X", ctypes.c_void_p), ("Wg", ctypes.c_void_p), ("Wu", ctypes.c_void_p),
+                ("Wd", ctypes.c_void_p), ("bg", ctypes.c_void_p), ("bu", ctypes.c_void_p),
+                ("bd", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("ldwi", ctypes.c_int64),
+                ("ldwd", ctypes.c_int64)]
+
+
+class GatedGradsC(ctypes.Structure):
+    _fields_ = [("dX", ctypes.c_void_p), ("dWg", ctypes.c_void_p), ("dWu", ctypes.c_void_p),
+                ("dWd", ctypes.c_void_p), ("dbg", ctypes.c_void_p), ("dbu", ctypes.c_void_p),
+                ("dbd", ctypes.c_void_p), ("lddx", ctypes.c_int64), ("lddwi", ctypes.c_int64),
+                ("lddwd", ctypes.c_int64)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("gt", ctypes.c_int32), ("decay", ctypes.c_float)]
+
+
+class AdamwOpts(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("grad_scale", ctypes.c_double), ("step", ctypes.c_int64),
+                ("state_bits", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 _c_i64 = ctypes.c_int64
@@ -147,6 +180,31 @@ def load(path: str = LIB_PATH):
         ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_double),
         ctypes.POINTER(ctypes.c_int32), _c_p, _c_p, _c_p, _c_p, ctypes.c_size_t, _c_p]
     lib.fd_beta_flow_cascade.restype = ctypes.c_int
+    lib.fd_layer_norm.argtypes = [_c_p, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p,
+                                  ctypes.c_int, ctypes.c_float, _c_p, _c_i64, _c_p, _c_p]
+    lib.fd_layer_norm.restype = ctypes.c_int
+    lib.fd_layer_norm_workspace_size.argtypes = [_c_i64, _c_i64]
+    lib.fd_layer_norm_workspace_size.restype = ctypes.c_size_t
+    lib.fd_layer_norm_backward.argtypes = [_c_p, _c_i64, _c_p, ctypes.c_int, _c_i64, _c_i64,
+                                           _c_i64, _c_p, ctypes.c_int, _c_p, _c_p, _c_i64, _c_p,
+                                           _c_i64, _c_p, _c_p, _c_p, ctypes.c_size_t, _c_p]
+    lib.fd_layer_norm_backward.restype = ctypes.c_int
+    lib.fd_gated_saved_size.argtypes = [ctypes.POINTER(GatedBlock)]
+    lib.fd_gated_saved_size.restype = ctypes.c_size_t
+    lib.fd_gated_workspace_size.argtypes = [ctypes.POINTER(GatedBlock), ctypes.c_int32]
+    lib.fd_gated_workspace_size.restype = ctypes.c_size_t
+    lib.fd_gated_forward.argtypes = [ctypes.POINTER(GatedBlock), _c_p, _c_i64, _c_p, _c_i64, _c_p,
+                                     ctypes.c_size_t, _c_p, ctypes.c_size_t, _c_p]
+    lib.fd_gated_forward.restype = ctypes.c_int
+    lib.fd_gated_backward.argtypes = [ctypes.POINTER(GatedBlock), _c_p, _c_i64, _c_p,
+                                      ctypes.c_size_t, ctypes.POINTER(GatedGradsC), _c_p,
+                                      ctypes.c_size_t, _c_p]
+    lib.fd_gated_backward.restype = ctypes.c_int
+    lib.fd_adamw_default_opts.argtypes = [ctypes.POINTER(AdamwOpts)]
+    lib.fd_adamw_default_opts.restype = None
+    lib.fd_adamw_step.argtypes = [ctypes.POINTER(AdamwTensor), _c_i64, ctypes.POINTER(AdamwOpts),
+                                  _c_p]
+    lib.fd_adamw_step.restype = ctypes.c_int
     lib.fd_last_error.argtypes = []
     lib.fd_last_error.restype = ctypes.c_char_p
     lib.fd_status_string.argtypes = [ctypes.c_int]
@@ -534,3 +592,294 @@ def fd_beta_flow_cascade(Xs: Sequence[torch.Tensor], k: int, b: int, alpha: floa
     return Flow([recs[i].as_dict() for i in range(nrec.value)], bx.value,
                 FLOW_EXIT.get(why.value, str(why.value)), [evals[i] for i in range(k)], evecs,
                 psi, st)
+
+
+# ---- a parametric extension of the coordinates ----
+
+
+def _net_dtype(t: torch.Tensor, what: str) -> int:
+    if t.dtype == torch.float32:
+        return FD_F32
+    if t.dtype == torch.bfloat16:
+        return FD_BF16
+    raise TypeError(f"{what} must be float32 or bfloat16, got {t.dtype}")
+
+
+def _net_matrix(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str) -> int:
+    """The leading dimension of a row-major rows x cols matrix."""
+    if not t.is_cuda:
+        raise ValueError("all tensors must live on the GPU")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{what} must be {rows} x {cols}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError(f"{what} must be row-major")
+    if rows > 1:
+        if ld < cols:
+            raise ValueError(f"{what} has overlapping rows")
+        return ld
+    return max(ld, cols)
+
+
+def _net_vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str):
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("all tensors must live on the GPU")
+    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{what} must be {n} contiguous values of {dtype}")
+    return t.data_ptr()
+
+
+def _net_workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+    if ws is not None and ws.numel() * ws.element_size() >= need:
+        return ws
+    return _workspace(need, device)
+
+
+def fd_layer_norm(X: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                  beta: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                  Y: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None
+                  ) -> "tuple[torch.Tensor, torch.Tensor]":
+    """(Y, stats): (x - mean) rstd gamma + beta of each row of X, and its (mean, rstd)."""
+    lib = load()
+    if X.dim() != 2:
+        raise ValueError("X must be N x D")
+    N, D = X.shape
+    xt = _net_dtype(X, "X")
+    ldx = _net_matrix(X, N, D, X.dtype, "X")
+    w = gamma if gamma is not None else beta
+    wdtype = X.dtype if w is None else w.dtype
+    wt = xt if w is None else _net_dtype(w, "gamma and beta")
+    pg = _net_vector(gamma, D, wdtype, "gamma")
+    pb = _net_vector(beta, D, wdtype, "beta")
+    if Y is None:
+        Y = torch.empty((N, D), dtype=X.dtype, device=X.device)
+    if stats is None:
+        stats = torch.empty((N, 2), dtype=torch.float32, device=X.device)
+    _net_matrix(stats, N, 2, torch.float32, "stats")
+    if not stats.is_contiguous():
+        raise ValueError("stats must be contiguous")
+    _check(lib.fd_layer_norm(X.data_ptr(), xt, N, D, ldx, pg, pb, wt, eps, Y.data_ptr(),
+                             _net_matrix(Y, N, D, X.dtype, "Y"), stats.data_ptr(),
+                             _stream(X.device)))
+    return Y, stats
+
+
+@dataclass
+class LayerNormGrads:
+    dX: torch.Tensor
+    dgamma: Optional[torch.Tensor]
+    dbeta: Optional[torch.Tensor]
+
+
+def fd_layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[torch.Tensor],
+                           stats: torch.Tensor, add: Optional[torch.Tensor] = None,
+                           weight_grads: bool = True, dX: Optional[torch.Tensor] = None,
+                           ws: Optional[torch.Tensor] = None) -> LayerNormGrads:
+    """Gradients of fd_layer_norm; `add`, a residual branch's gradient, is added to dX."""
+    lib = load()
+    if X.dim() != 2:
+        raise ValueError("X must be N x D")
+    N, D = X.shape
+    dev = X.device
+    xt = _net_dtype(X, "X")
+    ldx = _net_matrix(X, N, D, X.dtype, "X")
+    lddy = _net_matrix(dY, N, D, X.dtype, "dY")
+    ldadd = 0 if add is None else _net_matrix(add, N, D, X.dtype, "add")
+    wdtype = X.dtype if gamma is None else gamma.dtype
+    wt = xt if gamma is None else _net_dtype(gamma, "gamma")
+    pg = _net_vector(gamma, D, wdtype, "gamma")
+    _net_matrix(stats, N, 2, torch.float32, "stats")
+    if not stats.is_contiguous():
+        raise ValueError("stats must be contiguous")
+    if dX is None:
+        dX = torch.empty((N, D), dtype=X.dtype, device=dev)
+    lddx = _net_matrix(dX, N, D, X.dtype, "dX")
+    dgamma = torch.empty(D, dtype=wdtype, device=dev) if weight_grads else None
+    dbeta = torch.empty(D, dtype=wdtype, device=dev) if weight_grads else None
+    ws = _net_workspace(ws, lib.fd_layer_norm_workspace_size(N, D), dev)
+    _check(lib.fd_layer_norm_backward(
+        dY.data_ptr(), lddy, X.data_ptr(), xt, N, D, ldx, pg, wt, stats.data_ptr(),
+        None if add is None else add.data_ptr(), ldadd, dX.data_ptr(), lddx,
+        dgamma.data_ptr() if weight_grads else None, dbeta.data_ptr() if weight_grads else None,
+        ws.data_ptr(), ws.numel() * ws.element_size(), _stream(dev)))
+    return LayerNormGrads(dX, dgamma, dbeta)
+
+
+def _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act) -> GatedBlock:
+    if X.dim() != 2 or Wg.dim() != 2 or Wd.dim() != 2:
+        raise ValueError("X, Wg, Wu and Wd must be matrices")
+    if act not in FD_ACT:
+        raise ValueError(f"act must be one of {sorted(FD_ACT)}, got {act!r}")
+    N, D = X.shape
+    F, O = Wg.shape[0], Wd.shape[0]
+    t = X.dtype
+    code = _net_dtype(X, "X")
+    ldx = _net_matrix(X, N, D, t, "X")
+    ldwi = _net_matrix(Wg, F, D, t, "Wg")
+    if _net_matrix(Wu, F, D, t, "Wu") != ldwi:
+        raise ValueError("Wg and Wu must have the same leading dimension")
+    ldwd = _net_matrix(Wd, O, F, t, "Wd")
+    return GatedBlock(N, D, F, O, code, FD_ACT[act], X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(),
+                      Wd.data_ptr(), _net_vector(bg, F, t, "bg"), _net_vector(bu, F, t, "bu"),
+                      _net_vector(bd, O, t, "bd"), ldx, ldwi, ldwd)
+
+
+def fd_gated_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor,
+                     bg: Optional[torch.Tensor] = None, bu: Optional[torch.Tensor] = None,
+                     bd: Optional[torch.Tensor] = None, R: Optional[torch.Tensor] = None,
+                     act: str = "silu", save: bool = False, Y: Optional[torch.Tensor] = None,
+                     ws: Optional[torch.Tensor] = None
+                     ) -> "tuple[torch.Tensor, Optional[torch.Tensor]]":
+    """(Y, saved): Y = (act(X Wg^T + bg) * (X Wu^T + bu)) Wd^T + bd [+ R];
+    saved (with save) is what fd_gated_backward takes to spare computing the
+    inner activations again."""
+    lib = load()
+    b = _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act)
+    dev = X.device
+    if Y is None:
+        Y = torch.empty((b.N, b.O), dtype=X.dtype, device=dev)
+    ldy = _net_matrix(Y, b.N, b.O, X.dtype, "Y")
+    ldr = 0 if R is None else _net_matrix(R, b.N, b.O, X.dtype, "R")
+    saved, nsaved = None, 0
+    if save:
+        nsaved = lib.fd_gated_saved_size(b)
+        saved = _workspace(nsaved, dev)
+    need = lib.fd_gated_workspace_size(b, 0)
+    ws = _net_workspace(ws, need, dev)
+    _check(lib.fd_gated_forward(b, None if R is None else R.data_ptr(), ldr, Y.data_ptr(), ldy,
+                                saved.data_ptr() if save else None, nsaved, ws.data_ptr(),
+                                ws.numel() * ws.element_size(), _stream(dev)))
+    return Y, saved
+
+
+@dataclass
+class GatedGrads:
+    dX: Optional[torch.Tensor]
+    dWg: torch.Tensor
+    dWu: torch.Tensor
+    dWd: torch.Tensor
+    dbg: Optional[torch.Tensor]
+    dbu: Optional[torch.Tensor]
+    dbd: Optional[torch.Tensor]
+
+
+def fd_gated_backward(dY: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor,
+                      Wd: torch.Tensor, bg: Optional[torch.Tensor] = None,
+                      bu: Optional[torch.Tensor] = None, bd: Optional[torch.Tensor] = None,
+                      act: str = "silu", saved: Optional[torch.Tensor] = None,
+                      want_dx: bool = True, grads: Optional[GatedGrads] = None,
+                      ws: Optional[torch.Tensor] = None) -> GatedGrads:
+    """Gradients of fd_gated_forward (R's is dY itself), into `grads` where
+    given; a bias has one where it was given."""
+    lib = load()
+    b = _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act)
+    dev, t = X.device, X.dtype
+    lddy = _net_matrix(dY, b.N, b.O, t, "dY")
+    if grads is None:
+        def like(x):
+            return None if x is None else torch.empty(x.shape, dtype=t, device=dev)
+
+        grads = GatedGrads(like(X) if want_dx else None, like(Wg), like(Wu), like(Wd), like(bg),
+                           like(bu), like(bd))
+    g = grads
+    lddwi = _net_matrix(g.dWg, b.F, b.D, t, "dWg")
+    if _net_matrix(g.dWu, b.F, b.D, t, "dWu") != lddwi:
+        raise ValueError("dWg and dWu must have the same leading dimension")
+    c = GatedGradsC(None if g.dX is None else g.dX.data_ptr(), g.dWg.data_ptr(),
+                    g.dWu.data_ptr(), g.dWd.data_ptr(), _net_vector(g.dbg, b.F, t, "dbg"),
+                    _net_vector(g.dbu, b.F, t, "dbu"), _net_vector(g.dbd, b.O, t, "dbd"),
+                    0 if g.dX is None else _net_matrix(g.dX, b.N, b.D, t, "dX"), lddwi,
+                    _net_matrix(g.dWd, b.O, b.F, t, "dWd"))
+    nsaved = 0 if saved is None else saved.numel() * saved.element_size()
+    need = lib.fd_gated_workspace_size(b, 2 if saved is None else 1)
+    ws = _net_workspace(ws, need, dev)
+    _check(lib.fd_gated_backward(b, dY.data_ptr(), lddy,
+                                 None if saved is None else saved.data_ptr(), nsaved, c,
+                                 ws.data_ptr(), ws.numel() * ws.element_size(), _stream(dev)))
+    return grads
+
+
+@dataclass
+class AdamwState:
+    """Moments, a tensor per parameter: float32 m and v; or, with scales,
+    float8_e4m3fn m and v = the second moment's square root, and a float32 scale
+    for each 256 elements."""
+    m: "list[torch.Tensor]"
+    v: "list[torch.Tensor]"
+    m_scale: "Optional[list[torch.Tensor]]" = None
+    v_scale: "Optional[list[torch.Tensor]]" = None
+
+
+def fd_adamw_state(params: Sequence[torch.Tensor], bits: int = 32) -> AdamwState:
+    """Cleared states for a first step."""
+    if bits not in (32, 8):
+        raise ValueError("bits must be 32 or 8")
+
+    def zeros(dtype, per=1):
+        return [torch.zeros(-(-p.numel() // per), dtype=dtype, device=p.device) for p in params]
+
+    if bits == 32:
+        return AdamwState(zeros(torch.float32), zeros(torch.float32))
+    return AdamwState(zeros(torch.float8_e4m3fn), zeros(torch.float8_e4m3fn),
+                      zeros(torch.float32, 256), zeros(torch.float32, 256))
+
+
+@dataclass
+class AdamwPlan:
+    """The tensors of a step, checked once; it keeps them alive."""
+    tensors: "list"
+    table: "ctypes.Array"
+    bits: int
+    device: torch.device
+
+
+def fd_adamw_plan(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
+                  state: AdamwState, copies: Optional[Sequence[torch.Tensor]] = None,
+                  decay: Optional[Sequence[float]] = None) -> AdamwPlan:
+    """Tensors that fd_adamw_step updates: float32 params from float32 or
+    bfloat16 grads, optionally bfloat16 copies of the params, and a multiplier of
+    the weight decay for each (default 1)."""
+    n = len(params)
+    bits = 32 if state.m_scale is None else 8
+    lists = [params, grads, state.m, state.v]
+    lists += [] if bits == 32 else [state.m_scale, state.v_scale]
+    lists += [] if copies is None else [copies]
+    if any(len(x) != n for x in lists) or (decay is not None and len(decay) != n):
+        raise ValueError("one tensor for each parameter is wanted")
+    moment = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    table = (AdamwTensor * n)()
+    for i, p in enumerate(params):
+        size = p.numel()
+
+        def at(t, dtypes, what, count=size):
+            if not t.is_cuda:
+                raise ValueError("all tensors must live on the GPU")
+            if t.numel() != count or t.dtype not in dtypes or not t.is_contiguous():
+                raise ValueError(f"{what} of tensor {i} must be {count} contiguous values of "
+                                 f"{' or '.join(map(str, dtypes))}")
+            return t.data_ptr()
+
+        blocks = -(-size // 256)
+        table[i] = AdamwTensor(
+            at(p, (torch.float32,), "the parameters"),
+            at(grads[i], (torch.float32, torch.bfloat16), "the gradient"),
+            at(state.m[i], (moment,), "m"), at(state.v[i], (moment,), "v"),
+            None if bits == 32 else at(state.m_scale[i], (torch.float32,), "m_scale", blocks),
+            None if bits == 32 else at(state.v_scale[i], (torch.float32,), "v_scale", blocks),
+            None if copies is None else at(copies[i], (torch.bfloat16,), "the copy"), size,
+            FD_F32 if grads[i].dtype == torch.float32 else FD_BF16,
+            1.0 if decay is None else decay[i])
+    device = params[0].device if n else torch.device("cuda", torch.cuda.current_device())
+    return AdamwPlan([list(x) for x in lists], table, bits, device)
+
+
+def fd_adamw_step(plan: AdamwPlan, step: int, lr: float = 1e-3, beta1: float = 0.9,
+                  beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+                  grad_scale: float = 1.0) -> None:
+    """One AdamW step over the plan's tensors, in place; `step` counts from 1."""
+    o = AdamwOpts(lr, beta1, beta2, eps, weight_decay, grad_scale, step, plan.bits, 0)
+    _check(load().fd_adamw_step(plan.table, len(plan.table), o, _stream(plan.device)))

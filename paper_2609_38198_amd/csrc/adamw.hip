@@ -1,0 +1,275 @@
+// AdamW over many tensors in few launches, states in 32 or 8 bits.
+#include <algorithm>
+#include <cmath>
+
+#include "fd_guard.hpp"
+#include "net_common.hpp"
+
+namespace fd {
+namespace net {
+namespace {
+
+constexpr int BLOCK = 256;      // elements that share a scale, and threads of a workgroup
+constexpr int CHUNK = 4096;     // elements of a workgroup
+constexpr int TABLE = 48;       // tensors of a launch: the table travels in its arguments (4 KB at most)
+constexpr float E4M3_TOP = 448.f;
+constexpr float E4M3_LEAST = 0x1p-9f;
+constexpr float LEAST_TOP = 0x1p-100f;  // a block below this is stored as zeros
+
+struct Tensor {
+  float* p;
+  const void* g;
+  void* m;
+  void* v;
+  float *ms, *vs;
+  bf16* copy;
+  int64_t n;
+  int32_t gt;
+  float keep;      // 1 - lr wd
+};
+struct Table {
+  Tensor t[TABLE];
+  uint32_t first[TABLE + 1];  // a tensor's first workgroup
+  int32_t count;
+};
+struct Step {
+  float b1, nb1, b2, nb2, rate, root, eps, gscale;
+};
+
+// The tensor of a workgroup: the last one whose first workgroup is not after it.
+__device__ __forceinline__ int find_tensor(const Table& tb, uint32_t wg) {
+  int lo = 0, hi = tb.count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (tb.first[mid] <= wg) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ void load_grad(const Tensor& t, int64_t at, int valid, float* g) {
+  if (t.gt == FD_F32)
+    load_wide<4>(static_cast<const float*>(t.g) + at, valid, g);
+  else
+    load_wide<4>(static_cast<const bf16*>(t.g) + at, valid, g);
+}
+
+// The moments and the update of one element, in the order that the formulas
+// are written and without contraction: which of two neighbouring 8-bit values a
+// moment rounds to then does not depend on the compiler.
+__device__ __forceinline__ void update(const Step& s, float keep, float g, float& p, float& m,
+                                       float& v, float& r) {
+#pragma clang fp contract(off)
+  g = g * s.gscale;
+  m = s.b1 * m + s.nb1 * g;
+  v = s.b2 * v + s.nb2 * (g * g);
+  r = sqrtf(v);
+  p = p * keep - s.rate * m / (r * s.root + s.eps);
+}
+
+// Bound by memory: 28 bytes an element and 2 each for a bfloat16 gradient less
+// and a copy more; four elements of a lane are one 16-byte access of each array.
+__global__ __launch_bounds__(BLOCK) void adamw_kernel(Table tb, Step s) {
+  const int ti = find_tensor(tb, blockIdx.x);
+  const Tensor& t = tb.t[ti];
+  const int64_t base = int64_t(blockIdx.x - tb.first[ti]) * CHUNK;
+  float* M = static_cast<float*>(t.m);
+  float* V = static_cast<float*>(t.v);
+#pragma unroll
+  for (int j = 0; j < CHUNK / (BLOCK * 4); ++j) {
+    const int64_t at = base + (j * BLOCK + int(threadIdx.x)) * 4;
+    const int valid = int(min(int64_t(4), t.n - at));
+    if (valid <= 0) break;
+    float p[4], g[4], m[4], v[4], r;
+    load_wide<4>(t.p + at, valid, p);
+    load_grad(t, at, valid, g);
+    load_wide<4>(M + at, valid, m);
+    load_wide<4>(V + at, valid, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) update(s, t.keep, g[i], p[i], m[i], v[i], r);
+    store_wide<4>(t.p + at, valid, p);
+    store_wide<4>(M + at, valid, m);
+    store_wide<4>(V + at, valid, v);
+    if (t.copy != nullptr) store_wide<4>(t.copy + at, valid, p);
+  }
+}
+
+__device__ __forceinline__ void widen_e4m3(const unsigned char* q, int valid, float scale,
+                                           float* out) {
+  int w = 0;
+  if (valid >= 4) {
+    __builtin_memcpy(&w, q, 4);
+  } else {
+    for (int i = 0; i < valid; ++i) w |= int(q[i]) << (8 * i);
+  }
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
+  const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+  out[0] = lo[0] * scale;
+  out[1] = lo[1] * scale;
+  out[2] = hi[0] * scale;
+  out[3] = hi[1] * scale;
+}
+
+// Four values of a block whose largest finite magnitude is found over the wave;
+// returns the block's scale.
+template <bool ROOT>
+__device__ __forceinline__ float narrow_e4m3(const float* x, unsigned char* q, int valid) {
+#pragma clang fp contract(off)
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = fabsf(x[i]);
+    if (i < valid && a < INFINITY) top = fmaxf(top, a);
+  }
+  top = wave_max(top);
+  if (top < LEAST_TOP) top = 0.f;
+  const float inv = top > 0.f ? (1.0f / top) * E4M3_TOP : 0.f;
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i] = x[i] * inv;
+    if (ROOT && x[i] > 0.f && inv > 0.f) y[i] = fmaxf(y[i], E4M3_LEAST);
+    if (!(fabsf(x[i]) < INFINITY)) y[i] = NAN;
+  }
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  if (valid >= 4) {
+    __builtin_memcpy(q, &w, 4);
+  } else {
+    for (int i = 0; i < valid; ++i) q[i] = static_cast<unsigned char>(w >> (8 * i));
+  }
+  return top * (1.0f / E4M3_TOP);
+}
+
+// The 8-bit form: one wave takes the 256 elements that share a scale, so that
+// the new scale is a maximum over its lanes.  12 to 18 bytes an element.
+__global__ __launch_bounds__(BLOCK) void adamw_e4m3_kernel(Table tb, Step s) {
+  const int ti = find_tensor(tb, blockIdx.x);
+  const Tensor& t = tb.t[ti];
+  const int64_t base = int64_t(blockIdx.x - tb.first[ti]) * CHUNK;
+  unsigned char* M = static_cast<unsigned char*>(t.m);
+  unsigned char* V = static_cast<unsigned char*>(t.v);
+  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
+#pragma unroll
+  for (int j = 0; j < CHUNK / (BLOCK * 4); ++j) {
+    const int64_t block = base + (j * (BLOCK / WAVE) + wave) * BLOCK;
+    if (block >= t.n) break;  // the whole wave
+    const int64_t at = block + lane * 4;
+    const int valid = int(max(int64_t(0), min(int64_t(4), t.n - at)));
+    float p[4], g[4], m[4], v[4], r[4];
+    load_wide<4>(t.p + at, valid, p);
+    load_grad(t, at, valid, g);
+    widen_e4m3(M + at, valid, t.ms[block / BLOCK], m);
+    widen_e4m3(V + at, valid, t.vs[block / BLOCK], r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = r[i] * r[i];
+      update(s, t.keep, g[i], p[i], m[i], v[i], r[i]);
+    }
+    store_wide<4>(t.p + at, valid, p);
+    if (t.copy != nullptr) store_wide<4>(t.copy + at, valid, p);
+    const float ms = narrow_e4m3<false>(m, M + at, valid);
+    const float vs = narrow_e4m3<true>(r, V + at, valid);
+    if (lane == 0) {
+      t.ms[block / BLOCK] = ms;
+      t.vs[block / BLOCK] = vs;
+    }
+  }
+}
+
+}  // namespace
+}  // namespace net
+}  // namespace fd
+
+using namespace fd;
+using namespace fd::net;
+
+extern "C" {
+
+void fd_adamw_default_opts(fd_adamw_opts* o) {
+  if (o == nullptr) return;
+  *o = fd_adamw_opts{};
+  o->lr = 1e-3;
+  o->beta1 = 0.9;
+  o->beta2 = 0.999;
+  o->eps = 1e-8;
+  o->weight_decay = 0.01;
+  o->grad_scale = 1.0;
+  o->step = 1;
+  o->state_bits = 32;
+}
+
+fd_status fd_adamw_step(const fd_adamw_tensor* tensors, int64_t count, const fd_adamw_opts* opts,
+                        void* stream) {
+  return guarded([&] {
+    FD_REQUIRE(count >= 0 && (count == 0 || tensors != nullptr), FD_ERR_INVALID_ARG,
+               "bad tensor list");
+    fd_adamw_opts o;
+    fd_adamw_default_opts(&o);
+    if (opts != nullptr) o = *opts;
+    FD_REQUIRE(o.state_bits == 32 || o.state_bits == 8, FD_ERR_UNSUPPORTED,
+               "state_bits must be 32 or 8");
+    FD_REQUIRE(o.step >= 1, FD_ERR_INVALID_ARG, "step must be >= 1");
+    FD_REQUIRE(o.beta1 >= 0 && o.beta1 < 1 && o.beta2 >= 0 && o.beta2 < 1, FD_ERR_INVALID_ARG,
+               "beta1 and beta2 must be in [0, 1)");
+    FD_REQUIRE(std::isfinite(o.lr) && o.eps >= 0 && std::isfinite(o.eps) &&
+                   std::isfinite(o.weight_decay) && std::isfinite(o.grad_scale),
+               FD_ERR_INVALID_ARG, "lr, eps, weight_decay and grad_scale must be finite, eps >= 0");
+    const bool narrow_states = o.state_bits == 8;
+    for (int64_t i = 0; i < count; ++i) {
+      const fd_adamw_tensor& t = tensors[i];
+      FD_REQUIRE(t.n >= 0 && t.n <= int64_t(1) << 40, FD_ERR_INVALID_ARG, "tensor size out of range");
+      if (t.n == 0) continue;
+      check_dtype(t.gt, "gradient dtype");
+      FD_REQUIRE(t.p != nullptr && t.g != nullptr && t.m != nullptr && t.v != nullptr,
+                 FD_ERR_INVALID_ARG, "tensor with a NULL array");
+      FD_REQUIRE(!narrow_states || (t.m_scale != nullptr && t.v_scale != nullptr),
+                 FD_ERR_INVALID_ARG, "8-bit states need their scales");
+      FD_REQUIRE(std::isfinite(t.decay), FD_ERR_INVALID_ARG, "decay must be finite");
+      check_element_aligned(t.p, FD_F32, "p");
+      check_element_aligned(t.g, t.gt, "g");
+      if (t.copy != nullptr) check_element_aligned(t.copy, FD_BF16, "copy");
+      check_element_aligned(narrow_states ? t.m_scale : t.m, FD_F32, "m");
+      check_element_aligned(narrow_states ? t.v_scale : t.v, FD_F32, "v");
+    }
+    Step s;
+    s.b1 = float(o.beta1);
+    s.nb1 = float(1.0 - o.beta1);
+    s.b2 = float(o.beta2);
+    s.nb2 = float(1.0 - o.beta2);
+    s.rate = float(o.lr / (1.0 - std::pow(o.beta1, double(o.step))));
+    s.root = float(1.0 / std::sqrt(1.0 - std::pow(o.beta2, double(o.step))));
+    s.eps = float(o.eps);
+    s.gscale = float(o.grad_scale);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    // a launch takes TABLE tensors and 2^30 workgroups at most
+    constexpr int64_t MAX_GROUPS = int64_t(1) << 30;
+    Table tb{};
+    int64_t groups = 0;
+    auto flush = [&] {
+      if (tb.count == 0) return;
+      tb.first[tb.count] = uint32_t(groups);
+      if (narrow_states)
+        adamw_e4m3_kernel<<<dim3(unsigned(groups)), dim3(BLOCK), 0, st>>>(tb, s);
+      else
+        adamw_kernel<<<dim3(unsigned(groups)), dim3(BLOCK), 0, st>>>(tb, s);
+      FD_LAUNCH_CHECK();
+      tb.count = 0;
+      groups = 0;
+    };
+    for (int64_t i = 0; i < count; ++i) {
+      const fd_adamw_tensor& t = tensors[i];
+      if (t.n == 0) continue;
+      const int64_t need = ceil_div(t.n, CHUNK);
+      if (tb.count == TABLE || groups + need > MAX_GROUPS) flush();
+      Tensor& d = tb.t[tb.count];
+      d = Tensor{t.p,       t.g,       t.m, t.v, t.m_scale, t.v_scale, static_cast<bf16*>(t.copy),
+                 t.n, t.gt, float(1.0 - o.lr * o.weight_decay * double(t.decay))};
+      tb.first[tb.count] = uint32_t(groups);
+      ++tb.count;
+      groups += need;
+    }
+    flush();
+  });
+}
+
+}  // extern "C"

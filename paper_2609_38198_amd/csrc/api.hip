@@ -8,6 +8,7 @@
 #include <string>
 #include <vector>
 
+#include "fd_guard.hpp"
 #include "fd_internal.hpp"
 #include "fd_solver.hpp"
 
@@ -16,24 +17,6 @@ namespace fd {
 static thread_local std::string g_err;
 void set_error(const std::string& msg) { g_err = msg; }
 const char* get_error() { return g_err.c_str(); }
-
-template <class F>
-static fd_status guarded(F&& f) {
-  try {
-    f();
-    set_error("");
-    return FD_OK;
-  } catch (const Error& e) {
-    set_error(e.msg);
-    return e.status;
-  } catch (const std::exception& e) {
-    set_error(std::string("internal error: ") + e.what());
-    return FD_ERR_HIP;
-  } catch (...) {
-    set_error("internal error");
-    return FD_ERR_HIP;
-  }
-}
 
 constexpr int64_t MAX_POINTS = int64_t(1) << 30;
 
