@@ -18,6 +18,7 @@ constexpr int BK = 64;           // k of a tile: 128 bytes of a row, one cache l
 constexpr int MAX_SEGS = 12;     // stretches of k: two matrices x six plane pairs
 constexpr int PLANES = 3;
 constexpr int PAIRS = 6;
+constexpr int64_t MAX_LD = int64_t(1) << 22;  // a tile's byte offsets stay below 2^31
 
 // Sixteen bytes of zeros that lanes past the end of k read.
 __device__ __align__(16) const unsigned char zero_chunk[16] = {};
@@ -25,20 +26,33 @@ __device__ __align__(16) const unsigned char zero_chunk[16] = {};
 // One operand: up to two matrices (gate and up weights in the forward product).
 struct Operand {
   const bf16* p[MAX_SEGS];  // per stretch of k
-  int64_t ld;
+  int64_t ld;               // below MAX_LD
   int64_t rows;             // m (n) extent: rows, or columns in column order (a multiple of 8)
   int64_t k;                // k extent of a stretch (row order: a multiple of 8); beyond it reads zero
 };
 
-// 64 lanes x 16 bytes from each lane's own address into 1 KB of LDS at `to`
-// (wave-uniform), asynchronously: complete after a wait for vmcnt.  In assembly,
-// because the compiler would wait for every such load before any LDS read;
-// the write to M0 needs one wait state before its use.
+// 64 lanes x 16 bytes into 1 KB of LDS at `to` (wave-uniform), asynchronously:
+// complete after a wait for vmcnt.  In assembly, because the compiler would
+// wait for every such load before any LDS read; the write to M0 needs one
+// wait state before its use.  From each lane's byte offset to a uniform base, or from each
+// lane's own address.
+__device__ __forceinline__ void lds_load16(const char* base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(to), "v"(off), "s"(base)
+               : "memory");
+}
 __device__ __forceinline__ void lds_load16(const void* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :
                : "s"(to), "v"(from)
                : "memory");
+}
+
+// A value that is the same in every lane, in a scalar register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return int64_t(uint64_t(uint32_t(uniform(int(x >> 32)))) << 32 | uint32_t(uniform(int(x))));
 }
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
@@ -66,49 +80,51 @@ struct Tile {
   static constexpr int LOADS = BYTES / 16 / THREADS;  // of a thread
   static constexpr int CPR = COL ? EXT / 8 : 8;       // chunks per LDS row
   static_assert(BYTES % (16 * THREADS) == 0, "whole loads");
-  static_assert((THREADS / CPR) % (COL ? 16 : 8) == 0, "a thread's rows share their swizzle");
+  static_assert((THREADS / CPR) % 8 == 0, "whole rows");
 
-  int64_t off[LOADS];  // element offset of each load from a stretch's start, k tile 0
-  int kofs;            // row order: k of this thread's chunk; column order: of its first load
-  int64_t step;        // elements per k tile
+  uint32_t off[LOADS];  // byte offset of each load from the tile's corner
+  int kofs;             // row order: k of this thread's chunk; column order: of its first load
+  int64_t corner, step; // bytes from a stretch's start to the tile, and to the next k tile
 
   static __device__ __forceinline__ int swizzle(int k) {
     return CPR >= 16 ? ((k & 3) | ((k >> 3) & 1) << 2) : (k & 3);
   }
 
-  // r0: the tile's first row (column) of the operand.
+  // r0: the tile's first row (column) of the operand.  Rows past the edge read
+  // the last one, columns past it the tile's first: those results are dropped.
   __device__ __forceinline__ void init(const Operand& op, int64_t r0) {
     const int tid = threadIdx.x;
+    const int left = int(min(int64_t(EXT), op.rows - r0));
+    const uint32_t ld = uint32_t(op.ld);  // below MAX_LD: offsets fit 32 bits
     if (COL) {
-      const int k = tid / CPR, slot = tid % CPR;
-      const int chunk = slot ^ (swizzle(k) << 1);
-      int64_t c = r0 + chunk * 8;
-      if (c >= op.rows) c = r0;  // results past the edge are dropped
-      kofs = k;
-      step = BK * op.ld;
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) off[i] = int64_t(k + i * (THREADS / CPR)) * op.ld + c;
-    } else {
-      const int r = tid / 8, slot = tid % 8;
-      kofs = (slot ^ (r & 7)) * 8;
-      step = BK;
+      kofs = tid / CPR;
+      corner = r0 * 2;
+      step = BK * 2 * op.ld;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
-        int64_t row = r0 + r + i * (THREADS / 8);
-        if (row >= op.rows) row = op.rows - 1;
-        off[i] = row * op.ld + kofs;
+        const int k = kofs + i * (THREADS / CPR);
+        const int c = ((tid % CPR) ^ (swizzle(k) << 1)) * 8;
+        off[i] = (uint32_t(k) * ld + uint32_t(c < left ? c : 0)) * 2;
+      }
+    } else {
+      const int r = tid / 8;
+      kofs = ((tid % 8) ^ (r & 7)) * 8;
+      corner = r0 * op.ld * 2;
+      step = BK * 2;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int row = min(r + i * (THREADS / 8), left - 1);
+        off[i] = (uint32_t(row) * ld + uint32_t(kofs)) * 2;
       }
     }
   }
 
-  // Issues the loads of k tile kt of the stretch at p into LDS.
-  __device__ __forceinline__ void load(const bf16* p, int64_t kt, int64_t k, uint32_t lds) const {
+  // Issues the loads of the k tile at p (uniform), of which `left` k are there.
+  __device__ __forceinline__ void load(const char* p, int left, uint32_t lds) const {
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (threadIdx.x / WAVE) * (WAVE * 16));
-    p += kt * step;
-    const int64_t left = k - kt * BK;  // k still to come: uniform
     if (left >= BK) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) lds_load16(p + off[i], to + i * THREADS * 16);
+      for (int i = 0; i < LOADS; ++i) lds_load16(p, off[i], to + i * THREADS * 16);
     } else {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
@@ -277,25 +293,44 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
   int64_t tm, tn;
   int split;
   place(p, tm, tn, split);
-  const int64_t m0 = tm * BM, n0 = tn * BH;
+  const int64_t m0 = uniform(tm * BM), n0 = uniform(tn * BH);
   TA ta;
-  TB tb, tb2;
+  TB tb;
   ta.init(p.a, m0);
-  tb.init(p.b, n0);
-  if (EPI == GATE) tb2.init(p.b2, n0);
+  tb.init(p.b, n0);  // GATE: the up weights have the same shape
 
+  // where the next k tile comes from, in scalar registers
   const int64_t total = p.ktiles * p.segs;
-  const int64_t t0 = total * split / p.splits, t1 = total * (split + 1) / p.splits;
-  int seg = int(t0 / p.ktiles);
-  int64_t kt = t0 - seg * p.ktiles;
+  const int t0 = uniform(int(total * split / p.splits));
+  const int tiles = uniform(int(total * (split + 1) / p.splits)) - t0;
+  int seg = uniform(int(t0 / p.ktiles));
+  int kt = uniform(int(t0 - seg * p.ktiles));
+  const int ktiles = int(p.ktiles);
+  const char *pa = nullptr, *pb = nullptr, *pb2 = nullptr;
+  int lefta = 0, leftb = 0;
+  auto enter = [&] {  // the stretch seg at k tile kt
+    const int64_t a = kt * ta.step + ta.corner, b = kt * tb.step + tb.corner;
+    pa = reinterpret_cast<const char*>(uniform(reinterpret_cast<int64_t>(p.a.p[seg]) + a));
+    pb = reinterpret_cast<const char*>(uniform(reinterpret_cast<int64_t>(p.b.p[seg]) + b));
+    if (EPI == GATE)
+      pb2 = reinterpret_cast<const char*>(uniform(reinterpret_cast<int64_t>(p.b2.p[seg]) + b));
+    lefta = uniform(int(p.a.k - int64_t(kt) * BK));
+    leftb = uniform(int(p.b.k - int64_t(kt) * BK));
+  };
   const uint32_t base = lds_address(smem);
   auto issue = [&](uint32_t lds) {
-    ta.load(p.a.p[seg], kt, p.a.k, lds);
-    tb.load(p.b.p[seg], kt, p.b.k, lds + TA::BYTES);
-    if (EPI == GATE) tb2.load(p.b2.p[seg], kt, p.b2.k, lds + TA::BYTES + TB::BYTES);
-    if (++kt == p.ktiles) {
+    ta.load(pa, lefta, lds);
+    tb.load(pb, leftb, lds + TA::BYTES);
+    if (EPI == GATE) tb.load(pb2, leftb, lds + TA::BYTES + TB::BYTES);
+    if (++kt == ktiles) {
       kt = 0;
-      ++seg;
+      if (++seg < p.segs) enter();
+    } else {
+      pa += ta.step;
+      pb += tb.step;
+      if (EPI == GATE) pb2 += tb.step;
+      lefta -= BK;
+      leftb -= BK;
     }
   };
 
@@ -315,32 +350,69 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  if (t0 < t1) issue(base);
-  for (int64_t t = t0; t < t1; ++t) {
-    // tile t has landed, and every wave is done with the other buffer
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const int cur = int(t - t0) & 1;
-    if (t + 1 < t1) issue(base + (cur ^ 1) * BUF);
-    const char* sa = smem + cur * BUF;
+  // Fragments of k step ks of the tile in a buffer.
+  bf16x8 fa[2][FM], fb[2][FN];
+  auto read = [&](int into, int buf, int ks) {
+    const char* sa = smem + buf * BUF;
     const char* sb = sa + TA::BYTES;
 #pragma unroll
-    for (int ks = 0; ks < BK / 16; ++ks) {
-      bf16x8 fa[FM], fb[FN];
+    for (int i = 0; i < FM; ++i) fa[into][i] = TA::fragment(sa, wm * TM + i * 32, ks);
 #pragma unroll
-      for (int i = 0; i < FM; ++i) fa[i] = TA::fragment(sa, wm * TM + i * 32, ks);
+    for (int j = 0; j < FN; ++j) {
+      if (EPI == GATE && j >= FN / 2)
+        fb[into][j] = TB::fragment(sb + TB::BYTES, brow(j) - BN / 2, ks);
+      else
+        fb[into][j] = TB::fragment(sb, brow(j), ks);
+    }
+  };
+  auto multiply = [&](int from) {
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        if (EPI == GATE && j >= FN / 2)
-          fb[j] = TB::fragment(sb + TB::BYTES, brow(j) - BN / 2, ks);
-        else
-          fb[j] = TB::fragment(sb, brow(j), ks);
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[from][j], fa[from][i], acc[i][j], 0, 0, 0);
+  };
+
+  // The scheduler's order within a step: LDS reads evenly among the products.
+  auto interleave = [] {
+    constexpr int READS = FM * (ACOL ? 2 : 1) + FN * (BCOL ? 2 : 1), MULS = FM * FN;
+#pragma unroll
+    for (int i = 0; i < MULS; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, (READS + MULS - 1) / MULS, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    }
+  };
+
+  // Two LDS buffers and two sets of fragments.  The fragments of a k step are
+  // read while the matrix unit works on the step before; at a tile's last step
+  // every wave has its last fragments of the tile, so one barrier both shows the
+  // next tile (loaded during this one) and frees this buffer for the tile after.
+  constexpr int STEPS = BK / 16;
+  static_assert(STEPS % 2 == 0, "the fragment sets alternate");
+  if (tiles > 0) {
+    enter();
+    issue(base);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (tiles > 1) issue(base + BUF);
+    read(0, 0, 0);
+  }
+  for (int t = 0; t < tiles; ++t) {
+    const int cur = t & 1;
+#pragma unroll
+    for (int ks = 0; ks < STEPS; ++ks) {
+      if (ks + 1 < STEPS) {
+        read((ks + 1) & 1, cur, ks + 1);
+      } else if (t + 1 < tiles) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        read(0, cur ^ 1, 0);
+        if (t + 2 < tiles) issue(base + cur * BUF);
       }
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+      multiply(ks & 1);
+      interleave();
     }
   }
   __syncthreads();  // the buffers become the waves' staging slabs
@@ -451,8 +523,8 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
   }
 
   if (EPI == GRAD) {
-    float sums[2] = {0.f, 0.f};
-    static_assert(EPI != GRAD || CN <= WAVE, "a lane sums one column");
+    constexpr int SC = (CN + WAVE - 1) / WAVE;  // columns that a lane sums
+    float sums[2][SC] = {};
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
       const int64_t mb = m0 + wm * TM + i * 32;
@@ -488,7 +560,9 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
         wave_fence();
         if (what < 2 && p.colsum != nullptr && lane < CN)
           for (int r = 0; r < 32; ++r)
-            sums[what] += *reinterpret_cast<const float*>(slab + r * PITCH + lane * 4);
+#pragma unroll
+            for (int c = 0; c < SC; ++c)
+              sums[what][c] += *reinterpret_cast<const float*>(slab + r * PITCH + (lane + c * WAVE) * 4);
         bf16* to = what == 2 ? p.H : p.dGU + (what == 1 ? p.Fp : 0);
         const int64_t ld = what == 2 ? p.Fp : 2 * p.Fp, plane = what == 2 ? p.hplane : p.gplane;
         for (int r = lane / LPR; r < 32; r += RPP) {
@@ -500,10 +574,14 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
         wave_fence();
       }
     }
-    if (p.colsum != nullptr && lane < CN && nw + lane < p.Fp) {
-      float* s = p.colsum + (tm * WM + wm) * 2 * p.Fp + nw + lane;
-      s[0] = sums[0];
-      s[p.Fp] = sums[1];
+#pragma unroll
+    for (int c = 0; c < SC; ++c) {
+      const int64_t f = nw + lane + c * WAVE;
+      if (p.colsum != nullptr && lane < CN && f < p.Fp) {
+        float* s = p.colsum + (tm * WM + wm) * 2 * p.Fp + f;
+        s[0] = sums[0][c];
+        s[p.Fp] = sums[1][c];
+      }
     }
   }
 }
