@@ -11,7 +11,7 @@ namespace {
 
 constexpr int GROUP = 256;
 
-// ---------------------------------------------------------------- packing
+// ---------------------------------------------------------------- before
 // A matrix as bfloat16 planes with rows of a multiple of eight elements, zeros
 // past the end: what the product's 16-byte loads need of operands that are
 // float32, odd in width or not 16-byte aligned.
@@ -22,15 +22,50 @@ struct PackJob {
   int64_t plane;
   int64_t first;                // the job's first workgroup
 };
+// Up to five matrices to pack, then the partial column sums of one (dY):
+// workgroup y of `parts` adds its stretch of rows.
 constexpr int PACK_JOBS = 5;
 struct PackJobs {
   PackJob j[PACK_JOBS];
   int count = 0;
   int64_t groups = 0;
+  const void* sum = nullptr;
+  int64_t sum_ld, sum_rows, sum_cols, sum_parts;
+  float* sum_out;
 };
 
 template <class T>
-__global__ __launch_bounds__(GROUP) void pack_kernel(PackJobs jobs) {
+__device__ void column_sums(const PackJobs& jobs, int64_t id) {
+  __shared__ float sums[4][WAVE];
+  const int64_t cols = jobs.sum_cols, across = (cols + WAVE - 1) / WAVE;
+  const int64_t y = id / across, col = (id - y * across) * WAVE + threadIdx.x % WAVE;
+  const int r = threadIdx.x / WAVE;
+  const int64_t r0 = jobs.sum_rows * y / jobs.sum_parts, r1 = jobs.sum_rows * (y + 1) / jobs.sum_parts;
+  float s = 0.f;
+  if (col < cols) {
+    const T* p = static_cast<const T*>(jobs.sum) + col;
+    int64_t i = r0 + r;
+    for (; i + 12 < r1; i += 16) {
+      const float a = widen(p[i * jobs.sum_ld]), b = widen(p[(i + 4) * jobs.sum_ld]);
+      const float c = widen(p[(i + 8) * jobs.sum_ld]), d = widen(p[(i + 12) * jobs.sum_ld]);
+      s += (a + b) + (c + d);
+    }
+    for (; i < r1; i += 4) s += widen(p[i * jobs.sum_ld]);
+  }
+  sums[r][threadIdx.x % WAVE] = s;
+  __syncthreads();
+  if (r == 0 && col < cols) {
+    for (int i = 1; i < 4; ++i) s += sums[i][threadIdx.x];
+    jobs.sum_out[y * cols + col] = s;
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(GROUP) void before_kernel(PackJobs jobs) {
+  if (int64_t(blockIdx.x) >= jobs.groups) {
+    column_sums<T>(jobs, int64_t(blockIdx.x) - jobs.groups);
+    return;
+  }
   int i = 0;
   while (i + 1 < jobs.count && jobs.j[i + 1].first <= int64_t(blockIdx.x)) ++i;
   const PackJob& job = jobs.j[i];
@@ -43,63 +78,53 @@ __global__ __launch_bounds__(GROUP) void pack_kernel(PackJobs jobs) {
   write_planes<T>(job.dst + row * job.ldp + col, job.plane, x);
 }
 
-// ---------------------------------------------------------------- sums
-// Partial column sums of a matrix: workgroup (x, y) adds rows y, y + gridDim.y,
-// ... of columns x; in the order of the rows, so the total's order is fixed.
-template <class T>
-__global__ __launch_bounds__(GROUP) void column_sum_kernel(const T* A, int64_t lda, int64_t rows,
-                                                           int64_t cols, float* part) {
-  __shared__ float sums[4][WAVE];
-  const int c = threadIdx.x % WAVE, r = threadIdx.x / WAVE;
-  const int64_t col = int64_t(blockIdx.x) * WAVE + c;
-  float s = 0.f;
-  if (col < cols)
-    for (int64_t i = int64_t(blockIdx.y) * 4 + r; i < rows; i += int64_t(gridDim.y) * 4)
-      s += widen(A[i * lda + col]);
-  sums[r][c] = s;
-  __syncthreads();
-  if (r == 0 && col < cols) {
-    for (int i = 1; i < 4; ++i) s += sums[i][c];
-    part[int64_t(blockIdx.y) * cols + col] = s;
-  }
-}
+// ---------------------------------------------------------------- after
+// What is left once the products are done: the sums over the parts of split
+// contractions, and over partial column sums; each in one fixed order.
+struct SplitJob {
+  const float* part;
+  int splits;
+  int64_t M, N, ldp;
+  void* out[2];
+  int64_t ldo, half, rows;
+  const void *bias, *R;
+  int64_t ldr;
+  int64_t first;
+};
+struct ColumnJob {  // column c of the first `valid` of every `width` goes to out[c / width]
+  const float* part;
+  int64_t rows, ld, width, valid;
+  void* out[2];
+  int64_t first;
+};
+struct AfterJobs {
+  SplitJob s[GROUP_GEMMS];
+  ColumnJob c[2];
+  int splits = 0, columns = 0;
+  int64_t groups = 0;
+};
 
-// Sums over `rows` rows of float32 partial sums, ld apart; column c of the
-// first `valid` of every `width` goes to out[c / width].
+// C = the parts (+ bias + R): four columns of a row a thread.
 template <class T>
-__global__ __launch_bounds__(GROUP) void reduce_columns_kernel(const float* part, int64_t rows,
-                                                               int64_t ld, int64_t width,
-                                                               int64_t valid, T* out0, T* out1) {
-  __shared__ float sums[16][17];
-  const int c = threadIdx.x % 16, r = threadIdx.x / 16;
-  const int64_t col = int64_t(blockIdx.x) * 16 + c;
-  float s = 0.f;
-  if (col < ld)
-    for (int64_t i = r; i < rows; i += 16) s += part[i * ld + col];
-  sums[r][c] = s;
-  __syncthreads();
-  if (r != 0 || col >= ld) return;
-  for (int i = 1; i < 16; ++i) s += sums[i][c];
-  T* out = col < width ? out0 : out1;
-  const int64_t at = col < width ? col : col - width;
-  if (out != nullptr && at < valid) out[at] = narrow<T>(s);
-}
-
-// C = the splits' partial sums (+ bias + R), in the order of the splits.
-template <class T>
-__global__ __launch_bounds__(GROUP) void reduce_splits_kernel(const float* part, int splits,
-                                                              GemmArgs p) {
+__device__ void sum_splits(const SplitJob& p, int64_t id) {
   const int64_t per = (p.N + 3) / 4;
-  const int64_t at = int64_t(blockIdx.x) * GROUP + threadIdx.x;
+  const int64_t at = id * GROUP + threadIdx.x;
   const int64_t m = at / per, n = (at - m * per) * 4;
   if (m >= p.M) return;
   const int64_t row = m < p.half ? m : m - p.half;
-  if (row >= p.rows) return;
+  T* out = static_cast<T*>(p.out[m < p.half ? 0 : 1]);
+  if (row >= p.rows || out == nullptr) return;
   const int valid = int(min(int64_t(4), p.N - n));
-  const int64_t ldp = per * 4;
-  floatx4 s = *reinterpret_cast<const floatx4*>(part + m * ldp + n);
-  for (int i = 1; i < splits; ++i)
-    s += *reinterpret_cast<const floatx4*>(part + (i * p.M + m) * ldp + n);
+  const floatx4* q = reinterpret_cast<const floatx4*>(p.part + m * p.ldp + n);
+  const int64_t step = p.M * p.ldp / 4;
+  floatx4 s = {0.f, 0.f, 0.f, 0.f};
+  int i = 0;
+  for (; i + 4 <= p.splits; i += 4) {
+    const floatx4 a = q[i * step], b = q[(i + 1) * step], c = q[(i + 2) * step],
+                  d = q[(i + 3) * step];
+    s += (a + b) + (c + d);
+  }
+  for (; i < p.splits; ++i) s += q[i * step];
   float x[4] = {s[0], s[1], s[2], s[3]}, y[4];
   if (p.bias != nullptr) {
     load_wide<4>(static_cast<const T*>(p.bias) + n, valid, y);
@@ -109,8 +134,35 @@ __global__ __launch_bounds__(GROUP) void reduce_splits_kernel(const float* part,
     load_wide<4>(static_cast<const T*>(p.R) + m * p.ldr + n, valid, y);
     for (int e = 0; e < 4; ++e) x[e] += y[e];
   }
-  T* out = static_cast<T*>(p.out[m < p.half ? 0 : 1]);
-  if (out != nullptr) store_wide<4>(out + row * p.ldo + n, valid, x);
+  store_wide<4>(out + row * p.ldo + n, valid, x);
+}
+
+// Sixteen columns a workgroup, sixteen rows at a time.
+template <class T>
+__device__ void sum_columns(const ColumnJob& p, int64_t id) {
+  __shared__ float sums[16][17];
+  const int c = threadIdx.x % 16, r = threadIdx.x / 16;
+  const int64_t col = id * 16 + c;
+  float s = 0.f;
+  if (col < p.ld)
+    for (int64_t i = r; i < p.rows; i += 16) s += p.part[i * p.ld + col];
+  sums[r][c] = s;
+  __syncthreads();
+  if (r != 0 || col >= p.ld) return;
+  for (int i = 1; i < 16; ++i) s += sums[i][c];
+  T* out = static_cast<T*>(p.out[col < p.width ? 0 : 1]);
+  const int64_t at = col < p.width ? col : col - p.width;
+  if (out != nullptr && at < p.valid) out[at] = narrow<T>(s);
+}
+
+template <class T>
+__global__ __launch_bounds__(GROUP) void after_kernel(AfterJobs jobs) {
+  const int64_t id = blockIdx.x;
+  for (int i = jobs.columns - 1; i >= 0; --i)
+    if (id >= jobs.c[i].first) return sum_columns<T>(jobs.c[i], id - jobs.c[i].first);
+  int i = 0;
+  while (i + 1 < jobs.splits && jobs.s[i + 1].first <= id) ++i;
+  sum_splits<T>(jobs.s[i], id - jobs.s[i].first);
 }
 
 // Zero rows: weights' gradients are zero.
@@ -122,78 +174,228 @@ __global__ __launch_bounds__(GROUP) void clear_kernel(T* p, int64_t rows, int64_
 
 // ---------------------------------------------------------------- products
 
-// Tiles of C.  256 x 256 by eight waves of 128 x 64, one workgroup to a CU: the
-// LDS reads of a k step (96 bytes a clock at the matrix unit's full rate)
-// stay below its 128; 1,150 TFLOP/s at 16384 x 2048 x 8192 against 930 of four
-// waves of 128 x 128 and 840 of the 128 x 128 tile, whose 64 x 64 waves take all 128.  The smaller one
-// where the larger would leave CUs without a tile.
-constexpr int TILE = 128;
-constexpr int BIG_TILE = 256;
+// Tiles of C, by size: rows and columns of a tile, workgroups of a CU, and the
+// time of a k tile and of the rest of a tile (us, of one workgroup among as many as
+// fit) that plan() weighs them by.
+struct TileCost {
+  int bm, bn, per_cu;
+  double k, store, gate;  // gate: the epilogues of GATE and GRAD
+};
+enum { BIG = 0, MID = 1, SMALL = 2, CONFIGS = 3 };
 constexpr int64_t CUS = 256;
 
-// Parts of k: products with few tiles are split until two workgroups per CU
-// have work, at four k tiles each or more.
-int pick_splits(int64_t M, int64_t N, int64_t ktiles) {
-  const int64_t tiles = std::max<int64_t>(1, ceil_div(M, TILE) * ceil_div(N, TILE));
-  const int64_t want = 2 * CUS / tiles;
-  return int(std::max<int64_t>(1, std::min(want, ktiles / 4)));
+// bfloat16: 256 x 256 by eight waves of 128 x 64, whose LDS reads (96 bytes a
+// clock at the matrix unit's full rate) stay below the CU's 128; 128 x 128 by four waves of 64 x
+// 64, which take all of them; 64 x 64 by four waves of 32 x 32.
+// float32 (three planes): 256 x 128 and 128 x 128 by waves of 64 x 64 (64
+// bytes a clock), 64 x 64.
+template <class T>
+const TileCost* tile_costs() {
+  static const TileCost wide[CONFIGS] = {{256, 256, 1, 1.85, 8, 40}, {128, 128, 2, 1.2, 5, 16}, {64, 64, 4, 1.0, 3, 6}};
+  static const TileCost three[CONFIGS] = {{256, 128, 1, 3.4, 6, 30}, {128, 128, 1, 2.0, 5, 16}, {64, 64, 3, 1.3, 3, 6}};
+  return sizeof(T) == 4 ? three : wide;
 }
-size_t split_floats(int64_t M, int64_t N, int64_t ktiles) {
-  const int s = pick_splits(M, N, ktiles);
-  return s == 1 ? 0 : size_t(s) * size_t(M) * size_t(round_up(N, 4));
+
+template <int C, int EPI, class T>
+struct Config;  // BM, BN, WM, WN
+template <int EPI, class T> struct Config<BIG, EPI, T> { static constexpr int bm = 256, bn = sizeof(T) == 4 ? 128 : 256, wm = sizeof(T) == 4 ? 4 : 2, wn = sizeof(T) == 4 ? 2 : 4; };
+template <int EPI, class T> struct Config<MID, EPI, T> { static constexpr int bm = 128, bn = 128, wm = 2, wn = 2; };
+template <int EPI, class T> struct Config<SMALL, EPI, T> { static constexpr int bm = 64, bn = 64, wm = 2, wn = EPI == GATE ? 1 : 2; };
+
+// Extents and k tiles of a product, and how it is to run.
+struct Shape {
+  int64_t M = 0, N = 0, ktiles = 0;
+  int splits = 1;
+  size_t part() const { return splits == 1 ? 0 : size_t(splits) * size_t(M) * size_t(round_up(N, 4)); }
+};
+
+// The tile, and the parts of each product's k, of a launch of `count` products:
+// the least of an estimate that adds the rounds of workgroups (or the
+// longest one), and the traffic of the parts' sums.
+template <class T>
+int plan(Shape* s, int count, bool split, bool gate) {
+  const TileCost* costs = tile_costs<T>();
+  double best = 1e30;
+  int config = SMALL, best_cap = 0;
+  auto parts = [](int64_t ktiles, int64_t cap) { return cap == 0 ? 1 : int(std::max<int64_t>(1, ceil_div(ktiles, cap))); };
+  for (int c = 0; c < CONFIGS; ++c) {
+    const TileCost& t = costs[c];
+    for (int64_t cap : {0, 512, 256, 128, 64, 32, 16, 8, 4}) {
+      if (cap != 0 && !split) break;
+      double work = 0, longest = 0, sums = 0;
+      for (int i = 0; i < count; ++i) {
+        const int64_t tiles = ceil_div(s[i].M, t.bm) * ceil_div(s[i].N, t.bn);
+        const int n = parts(s[i].ktiles, cap);
+        const double one = double(s[i].ktiles) / n * t.k + (gate ? t.gate : t.store);
+        work += double(tiles) * n * one;
+        if (tiles > 0) longest = std::max(longest, one);
+        if (n > 1) sums += double(s[i].M) * double(s[i].N) * 4.0 * (2 * n + 1) / 4.0e6;  // us at 4 TB/s
+      }
+      const double slots = double(CUS * t.per_cu);
+      // whole rounds where they are few; averaged where many
+      const double rounds = work / slots;
+      const double time = std::max(rounds + 0.5 * longest, longest) + (sums > 0 ? sums + 4.0 : 0.0);
+      if (time < best) {
+        best = time;
+        config = c;
+        best_cap = int(cap);
+      }
+    }
+  }
+  for (int i = 0; i < count; ++i) s[i].splits = parts(s[i].ktiles, best_cap);
+  return config;
 }
 
 void check_grid(int64_t groups) {
   FD_REQUIRE(groups < (int64_t(1) << 31), FD_ERR_UNSUPPORTED, "problem too large for one launch");
 }
 
-template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, int EPI, class T, int ACT>
-void launch_config(GemmArgs& p, hipStream_t stream) {
-  constexpr int BH = EPI == GATE ? BN / 2 : BN;
-  constexpr size_t lds = 2 * (BM + BN) * BK * 2;
-  p.tiles_m = ceil_div(p.M, BM);
-  p.tiles_n = ceil_div(p.N, BH);
-  auto kernel = gemm_kernel<BM, BN, WM, WN, ACOL, BCOL, EPI, T, ACT>;
+template <class K>
+void allow_lds(K kernel, size_t bytes) {
   FD_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                   hipFuncAttributeMaxDynamicSharedMemorySize, int(lds)));
+                                   hipFuncAttributeMaxDynamicSharedMemorySize, int(bytes)));
+}
+
+template <int C, bool ACOL, bool BCOL, int EPI, class T, int ACT>
+void launch_config(GemmArgs& p, hipStream_t stream) {
+  using K = Config<C, EPI, T>;
+  constexpr size_t lds = gemm_lds<K::bm, K::bn, K::wm, K::wn, T>;
+  p.tiles_m = ceil_div(p.M, K::bm);
+  // GATE and GRAD write whole padded rows
+  p.tiles_n = ceil_div(EPI == STORE ? p.N : p.Fp, EPI == GATE ? K::bn / 2 : K::bn);
+  auto kernel = gemm_kernel<K::bm, K::bn, K::wm, K::wn, ACOL, BCOL, EPI, T, ACT>;
+  allow_lds(kernel, lds);
   check_grid(p.tiles_m * p.tiles_n * p.splits);
-  kernel<<<dim3(unsigned(p.tiles_m * p.tiles_n * p.splits)), dim3(WM * WN * WAVE), lds, stream>>>(p);
+  kernel<<<dim3(unsigned(p.tiles_m * p.tiles_n * p.splits)), dim3(K::wm * K::wn * WAVE), lds, stream>>>(p);
   FD_LAUNCH_CHECK();
 }
 
-bool big_tiles(int64_t M, int64_t N) {
-  return ceil_div(M, BIG_TILE) * ceil_div(N, BIG_TILE) >= CUS;
-}
-
 template <bool ACOL, bool BCOL, int EPI, class T, int ACT>
-void launch_tile(GemmArgs& p, hipStream_t stream) {
-  if (big_tiles(p.M, EPI == GATE ? 2 * p.N : p.N))
-    launch_config<BIG_TILE, BIG_TILE, 2, 4, ACOL, BCOL, EPI, T, ACT>(p, stream);
-  else
-    launch_config<TILE, TILE, 2, 2, ACOL, BCOL, EPI, T, ACT>(p, stream);
+void launch(int config, GemmArgs& p, hipStream_t stream) {
+  if (config == BIG) launch_config<BIG, ACOL, BCOL, EPI, T, ACT>(p, stream);
+  else if (config == MID) launch_config<MID, ACOL, BCOL, EPI, T, ACT>(p, stream);
+  else launch_config<SMALL, ACOL, BCOL, EPI, T, ACT>(p, stream);
 }
 
-// C stored as T, through partial sums where k is split.
-template <bool ACOL, bool BCOL, class T>
-void launch_store(GemmArgs& p, float* part, hipStream_t stream) {
-  p.splits = pick_splits(p.M, p.N, p.ktiles * p.segs);
-  if (p.splits == 1) {
-    launch_tile<ACOL, BCOL, STORE, T, 0>(p, stream);
-    return;
+template <int C, class T>
+void launch_group(GemmGroup& s, hipStream_t stream) {
+  using K = Config<C, STORE, T>;
+  constexpr size_t lds = gemm_lds<K::bm, K::bn, K::wm, K::wn, T>;
+  int64_t at = 0;
+  for (int i = 0; i < s.count; ++i) {
+    GemmArgs& p = s.g[i];
+    p.tiles_m = ceil_div(p.M, K::bm);
+    p.tiles_n = ceil_div(p.N, K::bn);
+    s.first[i] = at;
+    at += p.tiles_m * p.tiles_n * p.splits;
   }
-  GemmArgs q = p;
-  q.bias = q.R = nullptr;
-  q.out[0] = part;
-  q.ldo = round_up(p.N, 4);
-  q.half = q.rows = p.M;
-  launch_tile<ACOL, BCOL, STORE, float, 0>(q, stream);
-  const int64_t groups = ceil_div(p.M * ceil_div(p.N, 4), GROUP);
-  check_grid(groups);
-  reduce_splits_kernel<T><<<dim3(unsigned(groups)), dim3(GROUP), 0, stream>>>(part, p.splits, p);
+  s.first[s.count] = at;
+  check_grid(at);
+  auto kernel = gemm_group_kernel<K::bm, K::bn, K::wm, K::wn, T>;
+  allow_lds(kernel, lds);
+  kernel<<<dim3(unsigned(at)), dim3(K::wm * K::wn * WAVE), lds, stream>>>(s);
+  FD_LAUNCH_CHECK();
+}
+
+// A split product's parts, and their sum after it.
+void set_parts(GemmArgs& p, const Shape& s, float*& room, AfterJobs& after) {
+  p.splits = s.splits;
+  if (s.splits == 1) return;
+  p.part = room;
+  p.ldp = round_up(p.N, 4);
+  room += s.part();
+  SplitJob& j = after.s[after.splits++];
+  j = SplitJob{p.part, s.splits, p.M, p.N, p.ldp, {p.out[0], p.out[1]}, p.ldo, p.half, p.rows,
+               p.bias, p.R, p.ldr, after.groups};
+  after.groups += ceil_div(p.M * ceil_div(p.N, 4), GROUP);
+}
+void add_columns(AfterJobs& after, const float* part, int64_t rows, int64_t ld, int64_t width,
+                 int64_t valid, void* out0, void* out1) {
+  after.c[after.columns++] = ColumnJob{part, rows, ld, width, valid, {out0, out1}, after.groups};
+  after.groups += ceil_div(ld, 16);
+}
+template <class T>
+void run_after(const AfterJobs& after, hipStream_t stream) {
+  if (after.groups == 0) return;
+  check_grid(after.groups);
+  after_kernel<T><<<dim3(unsigned(after.groups)), dim3(GROUP), 0, stream>>>(after);
   FD_LAUNCH_CHECK();
 }
 
 // ---------------------------------------------------------------- the block
+
+struct Work {
+  bf16 *x = nullptr, *wg = nullptr, *wu = nullptr, *wd = nullptr, *dy = nullptr;
+  bf16 *h = nullptr, *dgu = nullptr;
+  float *part = nullptr, *colsum = nullptr, *dysum = nullptr;
+  char* saved = nullptr;
+  PackJobs jobs;
+  // the forward pass's Y, or the backward pass's dX, [dWg; dWu], dWd
+  Shape shapes[GROUP_GEMMS];
+  int config = SMALL;
+};
+
+int64_t f_padded(int64_t F) { return round_up(F, F_PAD); }
+
+template <class T>
+size_t packed(int64_t rows, int64_t cols) {
+  return size_t(rows) * size_t(round_up(cols, 8)) * planes_of<T>;
+}
+
+constexpr int64_t SUM_PARTS = 128;  // partial column sums of dY
+
+template <class T>
+size_t saved_bytes_t(int64_t N, int64_t F) {
+  return size_t(ceil_div(N, 32)) * size_t(f_padded(F) / 32) * saved_block_bytes<T>;
+}
+size_t saved_bytes(const fd_gated_block& b) {
+  return b.type == FD_F32 ? saved_bytes_t<float>(b.N, b.F) : saved_bytes_t<bf16>(b.N, b.F);
+}
+
+// Shapes of the products: Y; and dX, [dWg; dWu], dWd.
+template <class T>
+Shape shape_y(const fd_gated_block& b) {
+  return Shape{b.N, b.O, f_padded(b.F) / k_tile<T>};
+}
+template <class T>
+void shapes_grad(const fd_gated_block& b, Shape (&s)[GROUP_GEMMS]) {
+  const int64_t Fp = f_padded(b.F), nt = ceil_div(b.N, k_tile<T>);
+  s[0] = Shape{b.N, b.D, 2 * Fp / k_tile<T>};
+  s[1] = Shape{2 * Fp, b.D, nt};
+  s[2] = Shape{b.O, b.F, nt};
+}
+
+template <class T>
+Work carve_work_t(Arena& a, const fd_gated_block& b, int backward) {
+  Work w;
+  w.x = a.take<bf16>(packed<T>(b.N, b.D));
+  w.wg = a.take<bf16>(packed<T>(b.F, b.D));
+  w.wu = a.take<bf16>(packed<T>(b.F, b.D));
+  w.wd = a.take<bf16>(packed<T>(b.O, b.F));
+  const int64_t Fp = f_padded(b.F);
+  w.h = a.take<bf16>(size_t(b.N) * Fp * planes_of<T>);
+  size_t part = 0;
+  if (backward == 0) {
+    w.shapes[0] = shape_y<T>(b);
+    w.config = plan<T>(w.shapes, 1, true, false);
+    part = w.shapes[0].part();
+  } else {
+    w.dy = a.take<bf16>(packed<T>(b.N, b.O));
+    w.dgu = a.take<bf16>(size_t(b.N) * 2 * Fp * planes_of<T>);
+    // tiles of 64 or 128 rows have two rows of waves, of 256 rows at most four
+    w.colsum = a.take<float>(size_t(2 * ceil_div(b.N, 64) + 2) * 2 * Fp);
+    w.dysum = a.take<float>(size_t(SUM_PARTS) * size_t(b.O));
+    shapes_grad<T>(b, w.shapes);
+    w.config = plan<T>(w.shapes, GROUP_GEMMS, true, false);
+    for (const Shape& s : w.shapes) part += s.part();
+    if (backward == 2) w.saved = a.take<char>(saved_bytes(b));
+  }
+  w.part = a.take<float>(part);
+  return w;
+}
+Work carve_work(Arena& a, const fd_gated_block& b, int backward) {
+  return b.type == FD_F32 ? carve_work_t<float>(a, b, backward) : carve_work_t<bf16>(a, b, backward);
+}
 
 // A matrix operand in memory: as given where the product can load it, else packed.
 struct Matrix {
@@ -201,126 +403,59 @@ struct Matrix {
   int64_t ld = 0, rows = 0, cols = 0, plane = 0;  // cols: a multiple of 8
 };
 
-int planes_of(int type) { return type == FD_F32 ? PLANES : 1; }
-
-struct Work {
-  bf16 *x = nullptr, *wg = nullptr, *wu = nullptr, *wd = nullptr, *dy = nullptr;
-  bf16 *h = nullptr, *dgu = nullptr;
-  float *part = nullptr, *colsum = nullptr, *saved = nullptr;
-  PackJobs jobs;
-};
-
-int64_t f_padded(int64_t F) { return round_up(F, BK); }
-
-size_t packed(int64_t rows, int64_t cols, int type) {
-  return size_t(rows) * size_t(round_up(cols, 8)) * planes_of(type);
-}
-// k tiles of the contraction over n, and stretches of one matrix pair
-int segs_of(int type) { return type == FD_F32 ? PAIRS : 1; }
-
-constexpr int64_t SUM_ROWS = 64;  // row groups of dY's column sums
-size_t saved_floats(int64_t N, int64_t F) { return size_t(round_up(N, 32)) * f_padded(F) * 2; }
-
-Work carve_work(Arena& a, const fd_gated_block& b, int backward) {
-  Work w;
-  const int t = b.type, s = segs_of(t);
-  w.x = a.take<bf16>(packed(b.N, b.D, t));
-  w.wg = a.take<bf16>(packed(b.F, b.D, t));
-  w.wu = a.take<bf16>(packed(b.F, b.D, t));
-  w.wd = a.take<bf16>(packed(b.O, b.F, t));
-  const int64_t Fp = f_padded(b.F);
-  w.h = a.take<bf16>(size_t(b.N) * Fp * planes_of(t));
-  size_t part = 0;
-  if (backward == 0) {
-    part = split_floats(b.N, b.O, Fp / BK * s);
-  } else {
-    w.dy = a.take<bf16>(packed(b.N, b.O, t));
-    w.dgu = a.take<bf16>(size_t(b.N) * 2 * Fp * planes_of(t));
-    w.colsum = a.take<float>(std::max(size_t(ceil_div(b.N, TILE)) * 2 * 2 * Fp,
-                                      size_t(SUM_ROWS) * size_t(b.O)));
-    const int64_t nt = ceil_div(b.N, BK) * s;
-    part = std::max({split_floats(b.N, b.D, 2 * Fp / BK * s), split_floats(2 * Fp, b.D, nt),
-                     split_floats(b.O, b.F, nt)});
-    if (backward == 2) w.saved = a.take<float>(saved_floats(b.N, b.F));
-  }
-  w.part = a.take<float>(part);
-  return w;
-}
-
 bool direct(const void* p, int64_t ld, int64_t cols, int type) {
   return type == FD_BF16 && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 &&
          cols % 8 == 0 && ld < MAX_LD;
 }
 
-Matrix bring(Work& w, const void* p, int64_t ld, int64_t rows, int64_t cols, int type, bf16* room) {
-  if (direct(p, ld, cols, type)) return Matrix{static_cast<const bf16*>(p), ld, rows, cols, 0};
+Matrix pack(Work& w, const void* p, int64_t ld, int64_t rows, int64_t cols, bf16* room) {
   const int64_t ldp = round_up(cols, 8);
   PackJob& j = w.jobs.j[w.jobs.count++];
   j = PackJob{p, ld, rows, cols, ldp, room, rows * ldp, w.jobs.groups};
   w.jobs.groups += ceil_div(rows * (ldp / 8), GROUP);
   return Matrix{room, ldp, rows, ldp, rows * ldp};
 }
-
-void run_pack(const PackJobs& jobs, int type, hipStream_t stream) {
-  if (jobs.count == 0) return;
-  check_grid(jobs.groups);
-  if (type == FD_F32)
-    pack_kernel<float><<<dim3(unsigned(jobs.groups)), dim3(GROUP), 0, stream>>>(jobs);
-  else
-    pack_kernel<bf16><<<dim3(unsigned(jobs.groups)), dim3(GROUP), 0, stream>>>(jobs);
-  FD_LAUNCH_CHECK();
-}
-
-// The plane pairs of x y that reach 2^-24 of it, smallest first.
-constexpr int PAIR_A[PAIRS] = {1, 0, 2, 0, 1, 0};
-constexpr int PAIR_B[PAIRS] = {1, 2, 0, 1, 0, 0};
-
-// Stretches of matrix `which` (0 or 1 of those contracted one after the other).
-void set_rows(Operand& o, const Matrix& m, int type, int which, bool is_a, int64_t extent) {
-  const int s = segs_of(type);
-  for (int i = 0; i < s; ++i)
-    o.p[which * s + i] = m.p + (type == FD_F32 ? (is_a ? PAIR_A : PAIR_B)[i] * m.plane : 0);
-  o.ld = m.ld;
-  o.rows = extent;
-}
-
-Matrix view_h(const Work& w, const fd_gated_block& b) {
-  const int64_t Fp = f_padded(b.F);
-  return Matrix{w.h, Fp, b.N, Fp, b.N * Fp};
+Matrix bring(Work& w, const void* p, int64_t ld, int64_t rows, int64_t cols, int type, bf16* room) {
+  if (direct(p, ld, cols, type)) return Matrix{static_cast<const bf16*>(p), ld, rows, cols, 0};
+  return pack(w, p, ld, rows, cols, room);
 }
 
 template <class T>
-void by_act(const fd_gated_block& b, GemmArgs& p, int epi, hipStream_t st) {
-  p.splits = 1;
-  if (epi == GATE) {
-    if (b.act == FD_ACT_SILU) launch_tile<false, false, GATE, T, FD_ACT_SILU>(p, st);
-    else launch_tile<false, false, GATE, T, FD_ACT_GELU>(p, st);
-  } else {
-    if (b.act == FD_ACT_SILU) launch_tile<false, true, GRAD, T, FD_ACT_SILU>(p, st);
-    else launch_tile<false, true, GRAD, T, FD_ACT_GELU>(p, st);
-  }
+void run_before(const PackJobs& jobs, hipStream_t stream) {
+  const int64_t sums = jobs.sum == nullptr ? 0 : ceil_div(jobs.sum_cols, WAVE) * jobs.sum_parts;
+  const int64_t groups = jobs.groups + sums;
+  if (groups == 0) return;
+  check_grid(groups);
+  before_kernel<T><<<dim3(unsigned(groups)), dim3(GROUP), 0, stream>>>(jobs);
+  FD_LAUNCH_CHECK();
 }
+
+// Operand rows (columns where `col`) of a matrix.
+Operand rows_of(const Matrix& m) { return Operand{{m.p, nullptr}, m.ld, m.plane, m.rows, m.cols}; }
+Operand columns_of(const Matrix& m) { return Operand{{m.p, nullptr}, m.ld, m.plane, m.cols, m.rows}; }
 
 // G, U (kept where `saved`) and H (where `h`).
 template <class T>
 void run_gate(const fd_gated_block& b, const Work& w, const Matrix& x, const Matrix& wg,
-              const Matrix& wu, float* saved, bool h, hipStream_t st) {
+              const Matrix& wu, char* saved, bool h, hipStream_t st) {
   GemmArgs p{};
+  p.a = rows_of(x);
+  p.b = rows_of(wg);
+  p.up = wu.p;
   p.M = b.N;
   p.N = b.F;
-  p.segs = segs_of(b.type);
-  p.ktiles = ceil_div(x.cols, BK);
-  set_rows(p.a, x, b.type, 0, true, b.N);
-  set_rows(p.b, wg, b.type, 0, false, b.F);
-  set_rows(p.b2, wu, b.type, 0, false, b.F);
-  p.a.k = p.b.k = p.b2.k = x.cols;
+  p.segs = p.splits = 1;
+  p.ktiles = ceil_div(x.cols, k_tile<T>);
   p.bg = b.bg;
   p.bu = b.bu;
   p.saved = saved;
   p.Fp = f_padded(b.F);
   p.H = h ? w.h : nullptr;
   p.hplane = b.N * p.Fp;
-  by_act<T>(b, p, GATE, st);
+  Shape s{b.N, 2 * b.F, p.ktiles};
+  const int config = plan<T>(&s, 1, false, true);
+  if (b.act == FD_ACT_SILU) launch<false, false, GATE, T, FD_ACT_SILU>(config, p, st);
+  else launch<false, false, GATE, T, FD_ACT_GELU>(config, p, st);
 }
 
 void check_block(const fd_gated_block* bp) {
@@ -347,50 +482,66 @@ void check_arrays(const fd_gated_block& b) {
 
 void check_saved(const fd_gated_block& b, const void* saved, size_t bytes) {
   if (saved == nullptr) return;
-  FD_REQUIRE(bytes >= saved_floats(b.N, b.F) * sizeof(float), FD_ERR_WORKSPACE,
+  FD_REQUIRE(bytes >= saved_bytes(b), FD_ERR_WORKSPACE,
              "saved is too small");
   FD_REQUIRE((reinterpret_cast<uintptr_t>(saved) & 255) == 0, FD_ERR_WORKSPACE,
              "saved must be 256-byte aligned");
 }
 
 Work carve_checked(const fd_gated_block& b, int backward, void* ws, size_t ws_bytes) {
-  Arena m;
-  m.measuring = true;
-  carve_work(m, b, backward);
-  check_workspace(ws, ws_bytes, m.used);
+  check_workspace(ws, ws_bytes, 1);
   Arena a;
   a.base = static_cast<char*>(ws);
   a.cap = ws_bytes;
-  return carve_work(a, b, backward);
+  return carve_work(a, b, backward);  // throws where it does not fit
+}
+
+template <class T>
+int grad_wave_rows(int config) {
+  return config == BIG ? Config<BIG, GRAD, T>::wm : config == MID ? Config<MID, GRAD, T>::wm : Config<SMALL, GRAD, T>::wm;
+}
+
+// Both inner weights, laid out alike.
+void bring_weights(Work& w, const fd_gated_block& b, Matrix& wg, Matrix& wu) {
+  const int t = b.type;
+  if (direct(b.Wg, b.ldwi, b.D, t) && direct(b.Wu, b.ldwi, b.D, t)) {
+    wg = bring(w, b.Wg, b.ldwi, b.F, b.D, t, w.wg);
+    wu = bring(w, b.Wu, b.ldwi, b.F, b.D, t, w.wu);
+  } else {
+    wg = pack(w, b.Wg, b.ldwi, b.F, b.D, w.wg);
+    wu = pack(w, b.Wu, b.ldwi, b.F, b.D, w.wu);
+  }
 }
 
 template <class T>
 void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void* Y, int64_t ldy,
-             float* saved, hipStream_t st) {
+             char* saved, hipStream_t st) {
   const int t = b.type;
   const Matrix x = bring(w, b.X, b.ldx, b.N, b.D, t, w.x);
-  const Matrix wg = bring(w, b.Wg, b.ldwi, b.F, b.D, t, w.wg);
-  const Matrix wu = bring(w, b.Wu, b.ldwi, b.F, b.D, t, w.wu);
+  Matrix wg, wu;
+  bring_weights(w, b, wg, wu);
   const Matrix wd = bring(w, b.Wd, b.ldwd, b.O, b.F, t, w.wd);
-  run_pack(w.jobs, t, st);
+  run_before<T>(w.jobs, st);
   run_gate<T>(b, w, x, wg, wu, saved, true, st);
+  const int64_t Fp = f_padded(b.F);
   GemmArgs p{};
-  const Matrix h = view_h(w, b);
+  p.a = rows_of(Matrix{w.h, Fp, b.N, Fp, b.N * Fp});
+  p.b = rows_of(wd);
   p.M = b.N;
   p.N = b.O;
-  p.segs = segs_of(t);
-  p.ktiles = h.cols / BK;
-  set_rows(p.a, h, t, 0, true, b.N);
-  set_rows(p.b, wd, t, 0, false, b.O);
-  p.a.k = h.cols;
-  p.b.k = wd.cols;
+  p.segs = 1;
+  p.ktiles = Fp / k_tile<T>;
   p.out[0] = Y;
   p.ldo = ldy;
   p.half = p.rows = b.N;
   p.bias = b.bd;
   p.R = R;
   p.ldr = ldr;
-  launch_store<false, false, T>(p, w.part, st);
+  AfterJobs after;
+  float* room = w.part;
+  set_parts(p, w.shapes[0], room, after);
+  launch<false, false, STORE, T, 0>(w.config, p, st);
+  run_after<T>(after, st);
 }
 
 template <class T>
@@ -403,7 +554,7 @@ void clear(void* p, int64_t rows, int64_t cols, int64_t ld, hipStream_t st) {
 }
 
 template <class T>
-void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, const float* saved,
+void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, char* saved,
               const fd_gated_grads& g, hipStream_t st) {
   const int t = b.type;
   if (b.N == 0) {
@@ -418,108 +569,110 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, co
   const bool inner = g.dX != nullptr || g.dWg != nullptr || g.dWu != nullptr ||
                      g.dbg != nullptr || g.dbu != nullptr || g.dWd != nullptr;
   const int64_t Fp = f_padded(b.F);
+  const bool gate = inner && saved == nullptr;
+  const bool inner_weights = g.dWg != nullptr || g.dWu != nullptr;
+  Matrix x, wg, wu, wd, dy;
+  if (gate || inner_weights) x = bring(w, b.X, b.ldx, b.N, b.D, t, w.x);
+  if (gate || g.dX != nullptr) bring_weights(w, b, wg, wu);
   if (inner) {
-    const bool gate = saved == nullptr;
-    const bool need_x = gate || g.dWg != nullptr || g.dWu != nullptr;
-    const bool need_w = gate || g.dX != nullptr;
-    Matrix x, wg, wu;
-    if (need_x) x = bring(w, b.X, b.ldx, b.N, b.D, t, w.x);
-    if (need_w) {
-      wg = bring(w, b.Wg, b.ldwi, b.F, b.D, t, w.wg);
-      wu = bring(w, b.Wu, b.ldwi, b.F, b.D, t, w.wu);
-    }
-    const Matrix wd = bring(w, b.Wd, b.ldwd, b.O, b.F, t, w.wd);
-    const Matrix dy = bring(w, dY, lddy, b.N, b.O, t, w.dy);
-    run_pack(w.jobs, t, st);
+    wd = bring(w, b.Wd, b.ldwd, b.O, b.F, t, w.wd);
+    dy = bring(w, dY, lddy, b.N, b.O, t, w.dy);
+  }
+  AfterJobs after;
+  const int64_t parts = std::min<int64_t>(SUM_PARTS, ceil_div(b.N, 16));
+  if (g.dbd != nullptr) {
+    w.jobs.sum = dY;
+    w.jobs.sum_ld = lddy;
+    w.jobs.sum_rows = b.N;
+    w.jobs.sum_cols = b.O;
+    w.jobs.sum_parts = parts;
+    w.jobs.sum_out = w.dysum;
+  }
+  run_before<T>(w.jobs, st);
+  GemmGroup group{};
+  if (inner) {
     if (gate) {
       run_gate<T>(b, w, x, wg, wu, w.saved, false, st);
       saved = w.saved;
     }
-    {  // dH, and from it dG, dU, H
-      GemmArgs p{};
-      p.M = b.N;
-      p.N = b.F;
-      p.segs = segs_of(t);
-      p.ktiles = ceil_div(b.O, BK);
-      set_rows(p.a, dy, t, 0, true, b.N);
-      set_rows(p.b, wd, t, 0, false, wd.cols);
-      p.a.k = dy.cols;
-      p.b.k = b.O;
-      p.saved = const_cast<float*>(saved);
-      p.Fp = Fp;
-      p.H = w.h;
-      p.hplane = b.N * Fp;
-      p.dGU = w.dgu;
-      p.gplane = b.N * 2 * Fp;
-      p.colsum = g.dbg != nullptr || g.dbu != nullptr ? w.colsum : nullptr;
-      by_act<T>(b, p, GRAD, st);
-      if (p.colsum != nullptr) {
-        reduce_columns_kernel<T><<<dim3(unsigned(ceil_div(2 * Fp, 16))), dim3(GROUP), 0, st>>>(
-            w.colsum, p.tiles_m * 2, 2 * Fp, Fp, b.F, static_cast<T*>(g.dbg),
-            static_cast<T*>(g.dbu));
-        FD_LAUNCH_CHECK();
-      }
-    }
-    const Matrix h = view_h(w, b);
-    const Matrix dgu{w.dgu, 2 * Fp, b.N, 2 * Fp, b.N * 2 * Fp};
-    const Matrix du{w.dgu + Fp, 2 * Fp, b.N, Fp, b.N * 2 * Fp};
+    GemmArgs p{};  // dH, and from it dG, dU, H
+    p.a = rows_of(dy);
+    p.b = columns_of(wd);
+    p.M = b.N;
+    p.N = b.F;
+    p.segs = p.splits = 1;
+    p.ktiles = ceil_div(b.O, k_tile<T>);
+    p.saved = saved;
+    p.Fp = Fp;
+    p.H = w.h;
+    p.hplane = b.N * Fp;
+    p.dGU = w.dgu;
+    p.gplane = b.N * 2 * Fp;
+    p.colsum = g.dbg != nullptr || g.dbu != nullptr ? w.colsum : nullptr;
+    Shape s{b.N, b.F, p.ktiles};
+    const int config = plan<T>(&s, 1, false, true);
+    if (b.act == FD_ACT_SILU) launch<false, true, GRAD, T, FD_ACT_SILU>(config, p, st);
+    else launch<false, true, GRAD, T, FD_ACT_GELU>(config, p, st);
+    const int64_t wave_rows = p.tiles_m * grad_wave_rows<T>(config);
+
+    const Matrix h{w.h, Fp, b.N, Fp, b.N * Fp}, dgu{w.dgu, 2 * Fp, b.N, 2 * Fp, b.N * 2 * Fp};
+    Shape shapes[GROUP_GEMMS];
     if (g.dX != nullptr) {  // [dG dU] [Wg; Wu]
-      GemmArgs p{};
-      p.M = b.N;
-      p.N = b.D;
-      p.segs = 2 * segs_of(t);
-      p.ktiles = Fp / BK;
-      set_rows(p.a, dgu, t, 0, true, b.N);
-      set_rows(p.a, du, t, 1, true, b.N);
-      set_rows(p.b, wg, t, 0, false, wg.cols);
-      set_rows(p.b, wu, t, 1, false, wu.cols);
-      p.a.k = Fp;
-      p.b.k = b.F;
-      p.out[0] = g.dX;
-      p.ldo = g.lddx;
-      p.half = p.rows = b.N;
-      launch_store<false, true, T>(p, w.part, st);
+      GemmArgs& q = group.g[group.count];
+      q.a = rows_of(dgu);
+      q.a.k = Fp;
+      q.a.p[1] = w.dgu + Fp;
+      q.b = columns_of(wg);
+      q.b.p[1] = wu.p;
+      q.segs = 2;
+      q.ktiles = Fp / k_tile<T>;
+      q.out[0] = g.dX;
+      q.ldo = g.lddx;
+      q.half = q.rows = b.N;
+      shapes[group.count++] = w.shapes[0];
     }
-    if (g.dWg != nullptr || g.dWu != nullptr) {  // [dG dU]^T X
-      GemmArgs p{};
-      p.M = 2 * Fp;
-      p.N = b.D;
-      p.segs = segs_of(t);
-      p.ktiles = ceil_div(b.N, BK);
-      set_rows(p.a, dgu, t, 0, true, 2 * Fp);
-      set_rows(p.b, x, t, 0, false, x.cols);
-      p.a.k = p.b.k = b.N;
-      p.out[0] = g.dWg;
-      p.out[1] = g.dWu;
-      p.ldo = g.lddwi;
-      p.half = Fp;
-      p.rows = b.F;
-      launch_store<true, true, T>(p, w.part, st);
+    if (inner_weights) {  // [dG dU]^T X
+      GemmArgs& q = group.g[group.count];
+      q.a = columns_of(dgu);
+      q.b = columns_of(x);
+      q.segs = 1;
+      q.ktiles = ceil_div(b.N, k_tile<T>);
+      q.out[0] = g.dWg;
+      q.out[1] = g.dWu;
+      q.ldo = g.lddwi;
+      q.half = Fp;
+      q.rows = b.F;
+      group.acol[group.count] = true;
+      shapes[group.count++] = w.shapes[1];
     }
     if (g.dWd != nullptr) {  // dY^T H
-      GemmArgs p{};
-      p.M = b.O;
-      p.N = b.F;
-      p.segs = segs_of(t);
-      p.ktiles = ceil_div(b.N, BK);
-      set_rows(p.a, dy, t, 0, true, dy.cols);
-      set_rows(p.b, h, t, 0, false, h.cols);
-      p.a.k = p.b.k = b.N;
-      p.out[0] = g.dWd;
-      p.ldo = g.lddwd;
-      p.half = p.rows = b.O;
-      launch_store<true, true, T>(p, w.part, st);
+      GemmArgs& q = group.g[group.count];
+      q.a = columns_of(dy);
+      q.b = columns_of(h);
+      q.segs = 1;
+      q.ktiles = ceil_div(b.N, k_tile<T>);
+      q.out[0] = g.dWd;
+      q.ldo = g.lddwd;
+      q.half = q.rows = b.O;
+      group.acol[group.count] = true;
+      shapes[group.count++] = w.shapes[2];
     }
+    if (group.count > 0) {
+      float* room = w.part;
+      for (int i = 0; i < group.count; ++i) {
+        group.g[i].M = shapes[i].M;
+        group.g[i].N = shapes[i].N;
+        set_parts(group.g[i], shapes[i], room, after);
+      }
+      if (w.config == BIG) launch_group<BIG, T>(group, st);
+      else if (w.config == MID) launch_group<MID, T>(group, st);
+      else launch_group<SMALL, T>(group, st);
+    }
+    if (g.dbg != nullptr || g.dbu != nullptr)
+      add_columns(after, w.colsum, wave_rows, 2 * Fp, Fp, b.F, g.dbg, g.dbu);
   }
-  if (g.dbd != nullptr) {
-    const int64_t rows = std::min<int64_t>(SUM_ROWS, ceil_div(b.N, 4));
-    column_sum_kernel<T><<<dim3(unsigned(ceil_div(b.O, WAVE)), unsigned(rows)), dim3(GROUP), 0, st>>>(
-        static_cast<const T*>(dY), lddy, b.N, b.O, w.colsum);
-    FD_LAUNCH_CHECK();
-    reduce_columns_kernel<T><<<dim3(unsigned(ceil_div(b.O, 16))), dim3(GROUP), 0, st>>>(
-        w.colsum, rows, b.O, b.O, b.O, static_cast<T*>(g.dbd), nullptr);
-    FD_LAUNCH_CHECK();
-  }
+  if (g.dbd != nullptr) add_columns(after, w.dysum, parts, b.O, b.O, b.O, g.dbd, nullptr);
+  run_after<T>(after, st);
 }
 
 }  // namespace
@@ -535,7 +688,7 @@ size_t fd_gated_saved_size(const fd_gated_block* b) {
   size_t out = 0;
   const fd_status st = guarded([&] {
     check_block(b);
-    out = saved_floats(b->N, b->F) * sizeof(float);
+    out = saved_bytes(*b);
   });
   return st == FD_OK ? out : 0;
 }
@@ -570,9 +723,9 @@ fd_status fd_gated_forward(const fd_gated_block* b, const void* R, int64_t ldr, 
     Work w = carve_checked(*b, 0, ws, ws_bytes);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (b->type == FD_F32)
-      forward<float>(*b, w, R, ldr, Y, ldy, static_cast<float*>(saved), st);
+      forward<float>(*b, w, R, ldr, Y, ldy, static_cast<char*>(saved), st);
     else
-      forward<bf16>(*b, w, R, ldr, Y, ldy, static_cast<float*>(saved), st);
+      forward<bf16>(*b, w, R, ldr, Y, ldy, static_cast<char*>(saved), st);
   });
 }
 
@@ -598,9 +751,9 @@ fd_status fd_gated_backward(const fd_gated_block* b, const void* dY, int64_t ldd
     if (b->N > 0) w = carve_checked(*b, saved == nullptr ? 2 : 1, ws, ws_bytes);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (b->type == FD_F32)
-      backward<float>(*b, w, dY, lddy, static_cast<const float*>(saved), g, st);
+      backward<float>(*b, w, dY, lddy, static_cast<char*>(const_cast<void*>(saved)), g, st);
     else
-      backward<bf16>(*b, w, dY, lddy, static_cast<const float*>(saved), g, st);
+      backward<bf16>(*b, w, dY, lddy, static_cast<char*>(const_cast<void*>(saved)), g, st);
   });
 }
 

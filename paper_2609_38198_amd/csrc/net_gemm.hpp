@@ -4,9 +4,9 @@
 // Operands come in two orders: "rows" (k contiguous: p[m ld + k]) and "columns"
 // (m contiguous: p[k ld + m]), so that no operand is ever transposed in memory:
 // column tiles are transposed by the LDS read itself.  float32 operands enter
-// as three bfloat16 planes (x = x0 + x1 + x2 to 24 bits) and the contraction
-// runs over the six plane pairs whose product is above 2^-24 of x y, as if
-// they were further stretches of k.
+// as three bfloat16 planes (x = x0 + x1 + x2 to 24 bits); the six plane pairs whose
+// product reaches 2^-24 of x y are multiplied from one tile of all planes.  Six
+// products at the bfloat16 rate are 1.5 times the float32 unit's peak.
 #pragma once
 
 #include "net_common.hpp"
@@ -14,19 +14,21 @@
 namespace fd {
 namespace net {
 
-constexpr int BK = 64;           // k of a tile: 128 bytes of a row, one cache line
-constexpr int MAX_SEGS = 12;     // stretches of k: two matrices x six plane pairs
-constexpr int PLANES = 3;
-constexpr int PAIRS = 6;
-constexpr int64_t MAX_LD = int64_t(1) << 22;  // a tile's byte offsets stay below 2^31
+constexpr int F_PAD = 64;        // inner widths are padded to whole k tiles
+constexpr int MAX_SEGS = 2;      // matrices contracted one after the other
+template <class T>
+constexpr int planes_of = sizeof(T) == 4 ? 3 : 1;
+template <class T>
+constexpr int k_tile = sizeof(T) == 4 ? 32 : 64;  // k of an LDS tile
+constexpr int64_t MAX_LD = int64_t(1) << 22;      // a tile's byte offsets stay below 2^31
 
 // Sixteen bytes of zeros that lanes past the end of k read.
 __device__ __align__(16) const unsigned char zero_chunk[16] = {};
 
-// One operand: up to two matrices (gate and up weights in the forward product).
 struct Operand {
   const bf16* p[MAX_SEGS];  // per stretch of k
   int64_t ld;               // below MAX_LD
+  int64_t plane;            // elements between planes
   int64_t rows;             // m (n) extent: rows, or columns in column order (a multiple of 8)
   int64_t k;                // k extent of a stretch (row order: a multiple of 8); beyond it reads zero
 };
@@ -66,27 +68,31 @@ __device__ __forceinline__ bf16x4 lds_read_transposed(const char* p) {
   return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)p));
 }
 
-// LDS tile of EXT rows (columns) x BK, moved by THREADS threads.
+// LDS tile of EXT rows (columns) x KT of each of PL planes, moved by THREADS
+// threads.
 //
-// Row order: EXT rows of 128 bytes; 16-byte chunk c of row r is at slot
-// c ^ (r & 7), so that eight consecutive rows' same chunk cover all banks.
-// Column order: BK rows of 2 EXT bytes; 32-byte pair p of row k is at
+// Row order: EXT rows of 2 KT bytes; 16-byte chunk c of row r is at slot
+// c ^ (r & 7), or c ^ (r / 2 & 3) where a row is 64 bytes, so that eight consecutive rows'
+// same chunk cover all banks.
+// Column order: KT rows of 2 EXT bytes; 32-byte pair p of row k is at
 // p ^ s(k), s = k & 3 (and bit 3 of k as the next bit where a row has
 // eight pairs or more), so that the four rows which a transposing read of 16 lanes
 // takes at once lie in different banks.
-template <int EXT, int THREADS, bool COL>
+template <int EXT, int KT, int PL, int THREADS, bool COL>
 struct Tile {
-  static constexpr int BYTES = EXT * BK * 2;
-  static constexpr int LOADS = BYTES / 16 / THREADS;  // of a thread
-  static constexpr int CPR = COL ? EXT / 8 : 8;       // chunks per LDS row
-  static_assert(BYTES % (16 * THREADS) == 0, "whole loads");
-  static_assert((THREADS / CPR) % 8 == 0, "whole rows");
+  static constexpr int PLANE = EXT * KT * 2;
+  static constexpr int BYTES = PLANE * PL;
+  static constexpr int USED = PLANE / 16 < THREADS ? PLANE / 16 : THREADS;  // threads that load
+  static constexpr int LOADS = PLANE / 16 / USED;     // of a thread and plane
+  static constexpr int CPR = COL ? EXT / 8 : KT / 8;  // chunks per LDS row
+  static_assert(USED % WAVE == 0 && PLANE % (16 * USED) == 0 && USED % CPR == 0, "whole loads");
 
   uint32_t off[LOADS];  // byte offset of each load from the tile's corner
-  int kofs;             // row order: k of this thread's chunk; column order: of its first load
-  int64_t corner, step; // bytes from a stretch's start to the tile, and to the next k tile
+  int kofs[COL ? LOADS : 1];  // k of each load (row order: the same for all)
+  int64_t corner, step, plane;  // bytes from a stretch's start to the tile, to the next k tile, plane
 
-  static __device__ __forceinline__ int swizzle(int k) {
+  static __device__ __forceinline__ int row_swizzle(int r) { return KT == 64 ? r & 7 : r >> 1 & 3; }
+  static __device__ __forceinline__ int col_swizzle(int k) {
     return CPR >= 16 ? ((k & 3) | ((k >> 3) & 1) << 2) : (k & 3);
   }
 
@@ -94,49 +100,52 @@ struct Tile {
   // the last one, columns past it the tile's first: those results are dropped.
   __device__ __forceinline__ void init(const Operand& op, int64_t r0) {
     const int tid = threadIdx.x;
+    if (r0 >= op.rows) r0 = 0;  // a tile of padding alone
     const int left = int(min(int64_t(EXT), op.rows - r0));
     const uint32_t ld = uint32_t(op.ld);  // below MAX_LD: offsets fit 32 bits
-    if (COL) {
-      kofs = tid / CPR;
-      corner = r0 * 2;
-      step = BK * 2 * op.ld;
+    plane = op.plane * 2;
+    corner = COL ? r0 * 2 : r0 * op.ld * 2;
+    step = COL ? KT * 2 * op.ld : KT * 2;
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int k = kofs + i * (THREADS / CPR);
-        const int c = ((tid % CPR) ^ (swizzle(k) << 1)) * 8;
-        off[i] = (uint32_t(k) * ld + uint32_t(c < left ? c : 0)) * 2;
-      }
-    } else {
-      const int r = tid / 8;
-      kofs = ((tid % 8) ^ (r & 7)) * 8;
-      corner = r0 * op.ld * 2;
-      step = BK * 2;
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int row = min(r + i * (THREADS / 8), left - 1);
-        off[i] = (uint32_t(row) * ld + uint32_t(kofs)) * 2;
+    for (int i = 0; i < LOADS; ++i) {
+      const int r = (tid % USED + i * USED) / CPR, slot = tid % CPR;
+      if (COL) {
+        const int c = (slot ^ (col_swizzle(r) << 1)) * 8;
+        kofs[i] = r;
+        off[i] = (uint32_t(r) * ld + uint32_t(c < left ? c : 0)) * 2;
+      } else {
+        const int c = (slot ^ row_swizzle(r)) * 8;
+        if (i == 0) kofs[0] = c;
+        off[i] = (uint32_t(min(r, left - 1)) * ld + uint32_t(c)) * 2;
       }
     }
   }
+  static_assert(COL || LOADS == 1 || (USED / CPR) % 8 == 0, "one k for a thread's row loads");
 
   // Issues the loads of the k tile at p (uniform), of which `left` k are there.
   __device__ __forceinline__ void load(const char* p, int left, uint32_t lds) const {
-    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (threadIdx.x / WAVE) * (WAVE * 16));
-    if (left >= BK) {
+    uint32_t to = __builtin_amdgcn_readfirstlane(lds + (threadIdx.x / WAVE) * (WAVE * 16));
+    if (USED < THREADS && uniform(int(threadIdx.x)) >= USED) return;  // whole waves
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) lds_load16(p, off[i], to + i * THREADS * 16);
-    } else {
+    for (int q = 0; q < PL; ++q) {
+      if (left >= KT) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int at = COL ? kofs + i * (THREADS / CPR) : kofs;
-        const void* from = at < left ? static_cast<const void*>(p + off[i]) : zero_chunk;
-        lds_load16(from, to + i * THREADS * 16);
+        for (int i = 0; i < LOADS; ++i) lds_load16(p, off[i], to + i * USED * 16);
+      } else {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          const void* from =
+              kofs[COL ? i : 0] < left ? static_cast<const void*>(p + off[i]) : zero_chunk;
+          lds_load16(from, to + i * USED * 16);
+        }
       }
+      p += plane;
+      to += PLANE;
     }
   }
 
-  // The matrix operand of 32 rows (columns) from r0 on, k step ks: lane l has row
-  // l % 32, k = 16 ks + 8 (l / 32) + 0..7.
+  // The matrix operand of 32 rows (columns) from r0 on, k step ks, of the plane at
+  // lds: lane l has row l % 32, k = 16 ks + 8 (l / 32) + 0..7.
   static __device__ __forceinline__ bf16x8 fragment(const char* lds, int r0, int ks) {
     const int l = threadIdx.x % WAVE;
     if (COL) {
@@ -147,8 +156,8 @@ struct Tile {
       const bf16x4 lo = lds_read_transposed(p), hi = lds_read_transposed(p + 4 * EXT * 2);
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
-    const int row = r0 + l % 32, chunk = (ks * 2 + l / 32) ^ (l & 7);
-    return *reinterpret_cast<const bf16x8*>(lds + row * (BK * 2) + chunk * 16);
+    const int row = r0 + l % 32, chunk = (ks * 2 + l / 32) ^ row_swizzle(l % 32);
+    return *reinterpret_cast<const bf16x8*>(lds + row * (KT * 2) + chunk * 16);
   }
 };
 
@@ -208,38 +217,104 @@ enum Epilogue {
 };
 
 struct GemmArgs {
-  Operand a, b, b2;     // b2: GATE, the up weights
+  Operand a, b;
+  const bf16* up;       // GATE: the up weights, laid out as b's
   int64_t M, N;         // extents of C (GATE: N = F)
   int segs;             // stretches of k
   int64_t ktiles;       // k tiles of a stretch
   int splits;           // parts of the k tiles, each with its own workgroups
   int64_t tiles_m, tiles_n;
-  // STORE: row r of C goes to out[r / half], row r % half, if that is below `rows`
+  // STORE: row r of C goes to out[r / half], row r % half, if that is below
+  // `rows`; where k is split, all rows of split s go to part + s M ldp
   void* out[2];
   int64_t ldo, half, rows;
   const void *bias, *R;  // of type T, or NULL
   int64_t ldr;
+  float* part;
+  int64_t ldp;
   // GATE, GRAD
   const void *bg, *bu;  // of the block's type, or NULL
-  float* saved;         // G and U in fragment order, or NULL
-  int64_t Fp;           // F rounded up to BK: the planes' row length
+  char* saved;          // G and U by 32 x 32 blocks, or NULL
+  int64_t Fp;           // F rounded up to F_PAD: the planes' row length
   bf16 *H, *dGU;        // N x Fp, N x 2 Fp
   int64_t hplane, gplane;  // elements between planes
   float* colsum;        // 2 Fp column sums for each row of waves of each row tile, or NULL
-  int act;
 };
 
-// Where a 32 x 32 block of G starts in the kept buffer (U follows 1,024 floats
-// later): lane l's values 4 i .. 4 i + 3 are at (64 i + l) 4, 16 bytes a lane.
-__device__ __forceinline__ int64_t saved_block(int64_t m, int64_t f, int64_t Fp) {
-  return ((m / 32) * (Fp / 32) + f / 32) * 2048;
+// G and U are kept for the backward pass by 32 x 32 blocks in the accumulators'
+// own order, so that both sides move whole lines without a detour.  A float32
+// block keeps 4-byte values; a bfloat16 block 2-byte ones of 11 bits, scaled
+// by a power of two per block: 2^-12 of a value is lost, an eighth of what
+// the gradients' own rounding loses, for half of the bytes of the backward pass's
+// largest operand.
+template <class T>
+constexpr int64_t saved_block_bytes = sizeof(T) == 4 ? 8192 : 4096 + 16;
+
+template <class T>
+__device__ __forceinline__ char* saved_at(char* saved, int64_t m, int64_t f, int64_t Fp) {
+  return saved + ((m / 32) * (Fp / 32) + f / 32) * saved_block_bytes<T>;
+}
+
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+
+// One of a block's two arrays (which = 0: G, 1: U): lane l's values of a
+// quarter (float32) or half (bfloat16) of the block are 16 bytes at 16 l.
+template <class T>
+__device__ __forceinline__ void save16(char* block, int which, int lane, const floatx16& x) {
+  if (sizeof(T) == 4) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const floatx4 v = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+      *reinterpret_cast<floatx4*>(block + which * 4096 + (q * WAVE + lane) * 16) = v;
+    }
+    return;
+  }
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.f);
+  top = wave_max(top);
+  // 2^14 below the type's largest power, for blocks down to 2^-100
+  const int e = max(int(__builtin_bit_cast(uint32_t, top) >> 23), 27);
+  const float scale = __builtin_bit_cast(float, uint32_t(127 + 14 + 127 - e) << 23);
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    halfx8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = _Float16(x[8 * q + i] * scale);
+    *reinterpret_cast<halfx8*>(block + 16 + which * 2048 + (q * WAVE + lane) * 16) = v;
+  }
+  if (lane == 0)
+    *reinterpret_cast<float*>(block + which * 4) =
+        __builtin_bit_cast(float, uint32_t(e - 14) << 23);
+}
+template <class T>
+__device__ __forceinline__ floatx16 saved16(const char* block, int which, int lane) {
+  floatx16 x;
+  if (sizeof(T) == 4) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const floatx4 v = *reinterpret_cast<const floatx4*>(block + which * 4096 + (q * WAVE + lane) * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * q + i] = v[i];
+    }
+    return x;
+  }
+  const float scale = *reinterpret_cast<const float*>(block + which * 4);
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const halfx8 v = *reinterpret_cast<const halfx8*>(block + 16 + which * 2048 + (q * WAVE + lane) * 16);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[8 * q + i] = float(v[i]) * scale;
+  }
+  return x;
 }
 
 // XCD-aware order: workgroups go to the 8 XCDs in turn, so each XCD gets one
 // contiguous stretch of tiles; within it, groups of 8 row tiles walk the
 // columns together and share their operand tiles in that XCD's L2.
-__device__ __forceinline__ void place(const GemmArgs& p, int64_t& tm, int64_t& tn, int& split) {
-  const int64_t n = gridDim.x, id = blockIdx.x;
+__device__ __forceinline__ void place(const GemmArgs& p, int64_t id, int64_t& tm, int64_t& tn,
+                                      int& split) {
+  const int64_t n = p.tiles_m * p.tiles_n * p.splits;
   const int64_t q = n / 8, r = n % 8, x = id % 8;
   int64_t at = (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + id / 8;
   const int64_t per = p.tiles_m * p.tiles_n;
@@ -279,25 +354,30 @@ __device__ __forceinline__ void write_planes(bf16* p, int64_t plane, const float
 // instruction takes the n operand first, so that a lane holds four
 // consecutive n of one m: fragment value i is n = 8 (i / 4) + 4 (l / 32) + i % 4,
 // m = l % 32.
+//
+// id: the workgroup's number within the product.
+template <int BM, int BN, int WM, int WN, class T>
+constexpr size_t gemm_lds = 2 * (BM + BN) * k_tile<T> * 2 * planes_of<T>;
+
 template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, int EPI, class T, int ACT>
-__global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
-  constexpr int THREADS = WM * WN * WAVE;
+__device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* smem) {
+  constexpr int THREADS = WM * WN * WAVE, KT = k_tile<T>, PL = planes_of<T>;
   constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
   constexpr int BH = EPI == GATE ? BN / 2 : BN;  // extent of one b operand
-  using TA = Tile<BM, THREADS, ACOL>;
-  using TB = Tile<BH, THREADS, BCOL>;
-  constexpr int BUF = TA::BYTES + BN * BK * 2;
+  using TA = Tile<BM, KT, PL, THREADS, ACOL>;
+  using TB = Tile<BH, KT, PL, THREADS, BCOL>;
+  constexpr int BUF = TA::BYTES + TB::BYTES * (EPI == GATE ? 2 : 1);
+  static_assert(2 * BUF == gemm_lds<BM, BN, WM, WN, T>, "the launch's size");
   static_assert(EPI != GATE || FN % 2 == 0, "gate and up fragments in pairs");
-  extern __shared__ __align__(1024) char smem[];
 
   int64_t tm, tn;
   int split;
-  place(p, tm, tn, split);
+  place(p, id, tm, tn, split);
   const int64_t m0 = uniform(tm * BM), n0 = uniform(tn * BH);
   TA ta;
   TB tb;
   ta.init(p.a, m0);
-  tb.init(p.b, n0);  // GATE: the up weights have the same shape
+  tb.init(p.b, n0);
 
   // where the next k tile comes from, in scalar registers
   const int64_t total = p.ktiles * p.segs;
@@ -308,14 +388,16 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
   const int ktiles = int(p.ktiles);
   const char *pa = nullptr, *pb = nullptr, *pb2 = nullptr;
   int lefta = 0, leftb = 0;
+  auto at = [](const bf16* x, int64_t bytes) {
+    return reinterpret_cast<const char*>(uniform(reinterpret_cast<int64_t>(x) + bytes));
+  };
   auto enter = [&] {  // the stretch seg at k tile kt
-    const int64_t a = kt * ta.step + ta.corner, b = kt * tb.step + tb.corner;
-    pa = reinterpret_cast<const char*>(uniform(reinterpret_cast<int64_t>(p.a.p[seg]) + a));
-    pb = reinterpret_cast<const char*>(uniform(reinterpret_cast<int64_t>(p.b.p[seg]) + b));
-    if (EPI == GATE)
-      pb2 = reinterpret_cast<const char*>(uniform(reinterpret_cast<int64_t>(p.b2.p[seg]) + b));
-    lefta = uniform(int(p.a.k - int64_t(kt) * BK));
-    leftb = uniform(int(p.b.k - int64_t(kt) * BK));
+    const int64_t b = kt * tb.step + tb.corner;
+    pa = at(p.a.p[seg], kt * ta.step + ta.corner);
+    pb = at(p.b.p[seg], b);
+    if (EPI == GATE) pb2 = at(p.up, b);
+    lefta = uniform(int(p.a.k - int64_t(kt) * KT));
+    leftb = uniform(int(p.b.k - int64_t(kt) * KT));
   };
   const uint32_t base = lds_address(smem);
   auto issue = [&](uint32_t lds) {
@@ -329,19 +411,13 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
       pa += ta.step;
       pb += tb.step;
       if (EPI == GATE) pb2 += tb.step;
-      lefta -= BK;
-      leftb -= BK;
+      lefta -= KT;
+      leftb -= KT;
     }
   };
 
   const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
   const int wm = wave / WN, wn = wave % WN;
-  // first LDS row of n fragment f
-  auto brow = [&](int f) {
-    if (EPI == GATE)
-      return (f < FN / 2 ? 0 : BN / 2) + wn * (TN / 2) + (f % (FN / 2 > 0 ? FN / 2 : 1)) * 32;
-    return wn * TN + f * 32;
-  };
   floatx16 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
@@ -350,32 +426,42 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  // Fragments of k step ks of the tile in a buffer.
-  bf16x8 fa[2][FM], fb[2][FN];
+  // Fragments of k step ks of the tile in a buffer.  GATE: the first half of the n
+  // fragments are gate columns, the others the same up columns.
+  bf16x8 fa[2][PL][FM], fb[2][PL][FN];
   auto read = [&](int into, int buf, int ks) {
     const char* sa = smem + buf * BUF;
     const char* sb = sa + TA::BYTES;
 #pragma unroll
-    for (int i = 0; i < FM; ++i) fa[into][i] = TA::fragment(sa, wm * TM + i * 32, ks);
+    for (int q = 0; q < PL; ++q) {
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      if (EPI == GATE && j >= FN / 2)
-        fb[into][j] = TB::fragment(sb + TB::BYTES, brow(j) - BN / 2, ks);
-      else
-        fb[into][j] = TB::fragment(sb, brow(j), ks);
+      for (int i = 0; i < FM; ++i)
+        fa[into][q][i] = TA::fragment(sa + q * TA::PLANE, wm * TM + i * 32, ks);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        constexpr int HALF = EPI == GATE ? FN / 2 : FN;
+        fb[into][q][j] = TB::fragment(sb + (j / HALF) * TB::BYTES + q * TB::PLANE,
+                                      wn * HALF * 32 + (j % HALF) * 32, ks);
+      }
     }
   };
+  // The plane pairs of x y that reach 2^-24 of it, smallest first.
   auto multiply = [&](int from) {
+    constexpr int PAIRS = PL == 1 ? 1 : 6;
+    constexpr int PA[6] = {1, 0, 2, 0, 1, 0}, PB[6] = {1, 2, 0, 1, 0, 0};
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int q = 0; q < PAIRS; ++q)
 #pragma unroll
-      for (int j = 0; j < FN; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[from][j], fa[from][i], acc[i][j], 0, 0, 0);
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              fb[from][PL == 1 ? 0 : PB[q]][j], fa[from][PL == 1 ? 0 : PA[q]][i], acc[i][j], 0, 0, 0);
   };
-
   // The scheduler's order within a step: LDS reads evenly among the products.
   auto interleave = [] {
-    constexpr int READS = FM * (ACOL ? 2 : 1) + FN * (BCOL ? 2 : 1), MULS = FM * FN;
+    constexpr int READS = PL * (FM * (ACOL ? 2 : 1) + FN * (BCOL ? 2 : 1));
+    constexpr int MULS = FM * FN * (PL == 1 ? 1 : 6);
 #pragma unroll
     for (int i = 0; i < MULS; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x100, (READS + MULS - 1) / MULS, 0);
@@ -387,7 +473,7 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
   // read while the matrix unit works on the step before; at a tile's last step
   // every wave has its last fragments of the tile, so one barrier both shows the
   // next tile (loaded during this one) and frees this buffer for the tile after.
-  constexpr int STEPS = BK / 16;
+  constexpr int STEPS = KT / 16;
   static_assert(STEPS % 2 == 0, "the fragment sets alternate");
   if (tiles > 0) {
     enter();
@@ -445,15 +531,32 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
   const int64_t nw = n0 + wn * CN;          // the wave's first column
   const int64_t nl = nw + (lane % LPR) * 8;  // the lane's, on reading back
 
+  if (EPI == STORE && p.splits > 1) {
+    float* to = p.part + split * p.M * p.ldp;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) put(j, acc[i][j]);
+      wave_fence();
+      for (int r = lane / LPR; r < 32; r += RPP) {
+        const int64_t m = m0 + wm * TM + i * 32 + r;
+        if (m >= p.M || nl >= p.N) continue;
+        float x[8];
+        get(r, x);
+        store_wide<8>(to + m * p.ldp + nl, int(min(int64_t(8), p.N - nl)), x);
+      }
+      wave_fence();
+    }
+    return;
+  }
+
   if (EPI == STORE) {
+    const int valid = int(min(int64_t(8), p.N - nl));
     float bias[8];
     if (p.bias != nullptr && nl < p.N)
-      load_wide<8>(static_cast<const T*>(p.bias) + nl, int(min(int64_t(8), p.N - nl)), bias);
+      load_wide<8>(static_cast<const T*>(p.bias) + nl, valid, bias);
     else
       for (int e = 0; e < 8; ++e) bias[e] = 0.f;
-    T* o0 = static_cast<T*>(p.out[0]);
-    T* o1 = static_cast<T*>(p.out[1]);
-    if (p.splits > 1) o0 += split * p.M * p.ldo;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
 #pragma unroll
@@ -463,8 +566,8 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
         const int64_t m = m0 + wm * TM + i * 32 + r;
         if (m >= p.M || nl >= p.N) continue;
         const int64_t row = m < p.half ? m : m - p.half;
-        if (row >= p.rows) continue;
-        const int valid = int(min(int64_t(8), p.N - nl));
+        T* to = static_cast<T*>(p.out[m < p.half ? 0 : 1]);
+        if (row >= p.rows || to == nullptr) continue;
         float x[8], y[8];
         get(r, x);
 #pragma unroll
@@ -474,50 +577,72 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] += y[e];
         }
-        store_wide<8>((m < p.half ? o0 : o1) + row * p.ldo + nl, valid, x);
+        store_wide<8>(to + row * p.ldo + nl, valid, x);
       }
       wave_fence();
     }
   }
 
+  // Rows of planes from the slab.
+  auto write = [&](bf16* to, int64_t ld, int64_t plane, int64_t mb) {
+    for (int r = lane / LPR; r < 32; r += RPP) {
+      if (mb + r >= p.M || nl >= p.Fp) continue;
+      float x[8];
+      get(r, x);
+      write_planes<T>(to + (mb + r) * ld + nl, plane, x);
+    }
+  };
+
   if (EPI == GATE) {
+    constexpr int HALF = FN / 2 > 0 ? FN / 2 : 1;
+#pragma unroll
+    for (int j = 0; j < HALF; ++j) {
+      const int64_t fb = nw + j * 32;
+      float bg[16], bu[16];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t f = fb + 8 * q + 4 * half32;
+        const int valid = int(max(int64_t(0), min(int64_t(4), p.N - f)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bg[4 * q + e] = bu[4 * q + e] = 0.f;
+        if (p.bg != nullptr) load_wide<4>(static_cast<const T*>(p.bg) + f, valid, bg + 4 * q);
+        if (p.bu != nullptr) load_wide<4>(static_cast<const T*>(p.bu) + f, valid, bu + 4 * q);
+      }
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          acc[i][j][e] += bg[e];
+          acc[i][(j + HALF) % FN][e] += bu[e];
+        }
+      }
+    }
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
       const int64_t mb = m0 + wm * TM + i * 32;
+      if (mb >= p.M) break;
 #pragma unroll
-      for (int j = 0; j < FN / 2; ++j) {
+      for (int j = 0; j < HALF; ++j) {
         const int64_t fb = nw + j * 32;
+        const floatx16& g = acc[i][j];
+        const floatx16& u = acc[i][(j + HALF) % FN];
+        if (p.saved != nullptr && fb < p.Fp) {
+          char* block = saved_at<T>(p.saved, mb, fb, p.Fp);
+          save16<T>(block, 0, lane, g);
+          save16<T>(block, 1, lane, u);
+        }
+        if (p.H == nullptr) continue;
         floatx16 h;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int64_t f = fb + 8 * q + 4 * half32;
-          const int valid = int(max(int64_t(0), min(int64_t(4), p.N - f)));
-          float bg[4] = {0.f, 0.f, 0.f, 0.f}, bu[4] = {0.f, 0.f, 0.f, 0.f};
-          if (p.bg != nullptr) load_wide<4>(static_cast<const T*>(p.bg) + f, valid, bg);
-          if (p.bu != nullptr) load_wide<4>(static_cast<const T*>(p.bu) + f, valid, bu);
-          floatx4 g, u;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            g[e] = acc[i][j][4 * q + e] + bg[e];
-            u[e] = acc[i][j + FN / 2][4 * q + e] + bu[e];
-            h[4 * q + e] = e < valid ? activate<ACT>(g[e]).value * u[e] : 0.f;
-          }
-          if (p.saved != nullptr && mb < p.M && fb < p.Fp) {
-            float* s = p.saved + saved_block(mb, fb, p.Fp) + (q * WAVE + lane) * 4;
-            *reinterpret_cast<floatx4*>(s) = g;
-            *reinterpret_cast<floatx4*>(s + 1024) = u;
-          }
+        for (int e = 0; e < 16; ++e) {
+          const bool there = fb + 8 * (e / 4) + 4 * half32 + e % 4 < p.N;
+          h[e] = there ? activate<ACT>(g[e]).value * u[e] : 0.f;
         }
         put(j, h);
       }
       if (p.H == nullptr) continue;
       wave_fence();
-      for (int r = lane / LPR; r < 32; r += RPP) {
-        if (mb + r >= p.M || nl >= p.Fp) continue;
-        float x[8];
-        get(r, x);
-        write_planes<T>(p.H + (mb + r) * p.Fp + nl, p.hplane, x);
-      }
+      write(p.H, p.Fp, p.hplane, mb);
       wave_fence();
     }
   }
@@ -530,60 +655,81 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
       const int64_t mb = m0 + wm * TM + i * 32;
       if (mb >= p.M) break;
       const bool live = mb + lane % 32 < p.M;
+      floatx16 v[3][FN];  // dG, dU, H
 #pragma unroll
-      for (int what = 0; what < 3; ++what) {  // dG, dU, H
+      for (int j = 0; j < FN; ++j) {
+        const int64_t fb = nw + j * 32;
+        if (fb < p.Fp) {
+          const char* block = saved_at<T>(p.saved, mb, fb, p.Fp);
+          const floatx16 g = saved16<T>(block, 0, lane), u = saved16<T>(block, 1, lane);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          const int64_t fb = nw + j * 32;
-          floatx16 v;
-          if (fb < p.Fp) {
-            const float* s = p.saved + saved_block(mb, fb, p.Fp) + lane * 4;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const floatx4 g = *reinterpret_cast<const floatx4*>(s + q * WAVE * 4);
-              const floatx4 u = *reinterpret_cast<const floatx4*>(s + 1024 + q * WAVE * 4);
-              const int64_t f = fb + 8 * q + 4 * half32;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const Act a = activate<ACT>(g[e]);
-                const float dh = acc[i][j][4 * q + e];
-                const float x = what == 0 ? dh * u[e] * a.slope : what == 1 ? dh * a.value : a.value * u[e];
-                v[4 * q + e] = live && f + e < p.N ? x : 0.f;
-              }
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = 0.f;
+          for (int e = 0; e < 16; ++e) {
+            const bool there = live && fb + 8 * (e / 4) + 4 * half32 + e % 4 < p.N;
+            const Act a = activate<ACT>(g[e]);
+            const float dh = acc[i][j][e];
+            v[0][j][e] = there ? dh * u[e] * a.slope : 0.f;
+            v[1][j][e] = there ? dh * a.value : 0.f;
+            v[2][j][e] = there ? a.value * u[e] : 0.f;
           }
-          put(j, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[0][j][e] = v[1][j][e] = v[2][j][e] = 0.f;
         }
+      }
+#pragma unroll
+      for (int what = 0; what < 3; ++what) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) put(j, v[what][j]);
         wave_fence();
         if (what < 2 && p.colsum != nullptr && lane < CN)
           for (int r = 0; r < 32; ++r)
 #pragma unroll
             for (int c = 0; c < SC; ++c)
               sums[what][c] += *reinterpret_cast<const float*>(slab + r * PITCH + (lane + c * WAVE) * 4);
-        bf16* to = what == 2 ? p.H : p.dGU + (what == 1 ? p.Fp : 0);
-        const int64_t ld = what == 2 ? p.Fp : 2 * p.Fp, plane = what == 2 ? p.hplane : p.gplane;
-        for (int r = lane / LPR; r < 32; r += RPP) {
-          if (mb + r >= p.M || nl >= p.Fp) continue;
-          float x[8];
-          get(r, x);
-          write_planes<T>(to + (mb + r) * ld + nl, plane, x);
-        }
+        if (what == 2) write(p.H, p.Fp, p.hplane, mb);
+        else write(p.dGU + what * p.Fp, 2 * p.Fp, p.gplane, mb);
         wave_fence();
       }
     }
+    if (p.colsum != nullptr && lane < CN) {
 #pragma unroll
-    for (int c = 0; c < SC; ++c) {
-      const int64_t f = nw + lane + c * WAVE;
-      if (p.colsum != nullptr && lane < CN && f < p.Fp) {
+      for (int c = 0; c < SC; ++c) {
+        const int64_t f = nw + lane + c * WAVE;
+        if (f >= p.Fp) continue;
         float* s = p.colsum + (tm * WM + wm) * 2 * p.Fp + f;
         s[0] = sums[0][c];
         s[p.Fp] = sums[1][c];
       }
     }
   }
+}
+
+template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, int EPI, class T, int ACT>
+__global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
+  extern __shared__ __align__(1024) char smem[];
+  gemm_body<BM, BN, WM, WN, ACOL, BCOL, EPI, T, ACT>(p, blockIdx.x, smem);
+}
+
+// The backward pass's last products, which do not depend on each other, in one
+// launch: the workgroups of one fill what another leaves idle.
+constexpr int GROUP_GEMMS = 3;
+struct GemmGroup {
+  GemmArgs g[GROUP_GEMMS];
+  bool acol[GROUP_GEMMS];          // a in column order (b always is)
+  int64_t first[GROUP_GEMMS + 1];  // a product's first workgroup
+  int count;
+};
+
+template <int BM, int BN, int WM, int WN, class T>
+__global__ __launch_bounds__(WM * WN * WAVE) void gemm_group_kernel(GemmGroup s) {
+  extern __shared__ __align__(1024) char smem[];
+  int i = 0;
+  while (i + 1 < s.count && s.first[i + 1] <= int64_t(blockIdx.x)) ++i;
+  const int64_t id = int64_t(blockIdx.x) - s.first[i];
+  if (s.acol[i])
+    gemm_body<BM, BN, WM, WN, true, true, STORE, T, 0>(s.g[i], id, smem);
+  else
+    gemm_body<BM, BN, WM, WN, false, true, STORE, T, 0>(s.g[i], id, smem);
 }
 
 }  // namespace net
