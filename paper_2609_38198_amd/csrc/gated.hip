@@ -1,5 +1,6 @@
 // The gated feed-forward block, forward and backward.
 #include <algorithm>
+#include <cmath>
 
 #include "fd_guard.hpp"
 #include "fd_solver.hpp"
@@ -174,12 +175,14 @@ __global__ __launch_bounds__(GROUP) void clear_kernel(T* p, int64_t rows, int64_
 
 // ---------------------------------------------------------------- products
 
-// Tiles of C, by size: rows and columns of a tile, workgroups of a CU, and the
-// time of a k tile and of the rest of a tile (us, of one workgroup among as many as
-// fit) that plan() weighs them by.
+// Tiles of C and what they cost on an MI355X (us, measured at 256 to 16384 rows
+// x 512 to 2048 -> 2048 to 8192 and ragged ones): a k tile as a CU's share among as many workgroups
+// as fit (operands by rows; by columns, where small tiles read LDS in twice as many
+// instructions), a k tile of a workgroup alone, and the rest of a workgroup by
+// epilogue.
 struct TileCost {
   int bm, bn, per_cu;
-  double k, store, gate;  // gate: the epilogues of GATE and GRAD
+  double k[2], alone, rest[3];  // rest: STORE, GATE, GRAD
 };
 enum { BIG = 0, MID = 1, SMALL = 2, CONFIGS = 3 };
 constexpr int64_t CUS = 256;
@@ -191,8 +194,12 @@ constexpr int64_t CUS = 256;
 // bytes a clock), 64 x 64.
 template <class T>
 const TileCost* tile_costs() {
-  static const TileCost wide[CONFIGS] = {{256, 256, 1, 1.85, 8, 40}, {128, 128, 2, 1.2, 5, 16}, {64, 64, 4, 1.0, 3, 6}};
-  static const TileCost three[CONFIGS] = {{256, 128, 1, 3.4, 6, 30}, {128, 128, 1, 2.0, 5, 16}, {64, 64, 3, 1.3, 3, 6}};
+  static const TileCost wide[CONFIGS] = {{256, 256, 1, {1.9, 1.9}, 1.65, {5, 14, 28}},
+                                         {128, 128, 2, {0.56, 0.56}, 0.85, {4, 8, 14}},
+                                         {64, 64, 5, {0.20, 0.30}, 0.80, {3, 6, 8}}};
+  static const TileCost three[CONFIGS] = {{256, 128, 1, {2.7, 2.7}, 2.5, {6, 17, 40}},
+                                          {128, 128, 1, {1.65, 1.65}, 1.5, {5, 12, 22}},
+                                          {64, 64, 3, {0.50, 0.50}, 0.74, {3, 6, 9}}};
   return sizeof(T) == 4 ? three : wide;
 }
 
@@ -209,40 +216,55 @@ struct Shape {
   size_t part() const { return splits == 1 ? 0 : size_t(splits) * size_t(M) * size_t(round_up(N, 4)); }
 };
 
-// The tile, and the parts of each product's k, of a launch of `count` products:
-// the least of an estimate that adds the rounds of workgroups (or the
-// longest one), and the traffic of the parts' sums.
+// The tile, and the parts of each product's k (with `split`), of a launch of
+// `count` products: the least of an estimate that counts whole rounds of a
+// workgroup a CU, the longest workgroup, and the traffic of the parts' sums.
 template <class T>
-int plan(Shape* s, int count, bool split, bool gate) {
+int plan(Shape* s, int count, bool split, int epilogue, bool columns) {
   const TileCost* costs = tile_costs<T>();
   double best = 1e30;
-  int config = SMALL, best_cap = 0;
-  auto parts = [](int64_t ktiles, int64_t cap) { return cap == 0 ? 1 : int(std::max<int64_t>(1, ceil_div(ktiles, cap))); };
+  int config = SMALL;
+  int parts[GROUP_GEMMS] = {1, 1, 1};
   for (int c = 0; c < CONFIGS; ++c) {
     const TileCost& t = costs[c];
-    for (int64_t cap : {0, 512, 256, 128, 64, 32, 16, 8, 4}) {
-      if (cap != 0 && !split) break;
-      double work = 0, longest = 0, sums = 0;
-      for (int i = 0; i < count; ++i) {
-        const int64_t tiles = ceil_div(s[i].M, t.bm) * ceil_div(s[i].N, t.bn);
-        const int n = parts(s[i].ktiles, cap);
-        const double one = double(s[i].ktiles) / n * t.k + (gate ? t.gate : t.store);
-        work += double(tiles) * n * one;
-        if (tiles > 0) longest = std::max(longest, one);
-        if (n > 1) sums += double(s[i].M) * double(s[i].N) * 4.0 * (2 * n + 1) / 4.0e6;  // us at 4 TB/s
-      }
-      const double slots = double(CUS * t.per_cu);
-      // whole rounds where they are few; averaged where many
-      const double rounds = work / slots;
-      const double time = std::max(rounds + 0.5 * longest, longest) + (sums > 0 ? sums + 4.0 : 0.0);
-      if (time < best) {
-        best = time;
-        config = c;
-        best_cap = int(cap);
+    const double rest = t.rest[epilogue];
+    double tiles[GROUP_GEMMS], k[GROUP_GEMMS], mn[GROUP_GEMMS];
+    for (int i = 0; i < count; ++i) {
+      tiles[i] = double(ceil_div(s[i].M, t.bm) * ceil_div(s[i].N, t.bn));
+      k[i] = double(s[i].ktiles);
+      mn[i] = double(s[i].M) * double(s[i].N);
+    }
+    for (int cap = split ? 4 : 1024; cap <= 1024; cap *= 2) {
+      // of the products longer than the cap, those in the mask are split
+      for (int mask = 0; mask < (split ? 1 << count : 1); ++mask) {
+        double groups = 0, work = 0, longest = 0, sums = 0;
+        int n[GROUP_GEMMS];
+        bool fresh = true;
+        for (int i = 0; i < count; ++i) {
+          n[i] = 1;
+          if (mask >> i & 1) {
+            if (s[i].ktiles <= cap) fresh = false;  // the same as without it
+            n[i] = int(std::max<int64_t>(1, ceil_div(s[i].ktiles, int64_t(cap))));
+          }
+          const double each = k[i] / n[i];
+          groups += tiles[i] * n[i];
+          work += tiles[i] * n[i] * (each * t.k[columns] + rest / t.per_cu);
+          longest = std::max(longest, each * t.alone + rest);
+          if (n[i] > 1) sums += mn[i] * 4.0 * (2 * n[i] + 1) / 4.0e6;  // 4 TB/s
+        }
+        if (!fresh) continue;
+        const double rounds = groups / double(CUS);
+        const double time = std::max(work / double(CUS) * std::ceil(rounds) / std::max(rounds, 1e-9), longest) +
+                            (sums > 0 ? sums + 4.0 : 0.0);
+        if (time < best) {
+          best = time;
+          config = c;
+          for (int i = 0; i < count; ++i) parts[i] = n[i];
+        }
       }
     }
   }
-  for (int i = 0; i < count; ++i) s[i].splits = parts(s[i].ktiles, best_cap);
+  for (int i = 0; i < count; ++i) s[i].splits = parts[i];
   return config;
 }
 
@@ -377,7 +399,7 @@ Work carve_work_t(Arena& a, const fd_gated_block& b, int backward) {
   size_t part = 0;
   if (backward == 0) {
     w.shapes[0] = shape_y<T>(b);
-    w.config = plan<T>(w.shapes, 1, true, false);
+    w.config = plan<T>(w.shapes, 1, true, STORE, false);
     part = w.shapes[0].part();
   } else {
     w.dy = a.take<bf16>(packed<T>(b.N, b.O));
@@ -386,7 +408,7 @@ Work carve_work_t(Arena& a, const fd_gated_block& b, int backward) {
     w.colsum = a.take<float>(size_t(2 * ceil_div(b.N, 64) + 2) * 2 * Fp);
     w.dysum = a.take<float>(size_t(SUM_PARTS) * size_t(b.O));
     shapes_grad<T>(b, w.shapes);
-    w.config = plan<T>(w.shapes, GROUP_GEMMS, true, false);
+    w.config = plan<T>(w.shapes, GROUP_GEMMS, true, STORE, true);
     for (const Shape& s : w.shapes) part += s.part();
     if (backward == 2) w.saved = a.take<char>(saved_bytes(b));
   }
@@ -453,7 +475,7 @@ void run_gate(const fd_gated_block& b, const Work& w, const Matrix& x, const Mat
   p.H = h ? w.h : nullptr;
   p.hplane = b.N * p.Fp;
   Shape s{b.N, 2 * b.F, p.ktiles};
-  const int config = plan<T>(&s, 1, false, true);
+  const int config = plan<T>(&s, 1, false, GATE, false);
   if (b.act == FD_ACT_SILU) launch<false, false, GATE, T, FD_ACT_SILU>(config, p, st);
   else launch<false, false, GATE, T, FD_ACT_GELU>(config, p, st);
 }
@@ -610,7 +632,7 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
     p.gplane = b.N * 2 * Fp;
     p.colsum = g.dbg != nullptr || g.dbu != nullptr ? w.colsum : nullptr;
     Shape s{b.N, b.F, p.ktiles};
-    const int config = plan<T>(&s, 1, false, true);
+    const int config = plan<T>(&s, 1, false, GRAD, true);
     if (b.act == FD_ACT_SILU) launch<false, true, GRAD, T, FD_ACT_SILU>(config, p, st);
     else launch<false, true, GRAD, T, FD_ACT_GELU>(config, p, st);
     const int64_t wave_rows = p.tiles_m * grad_wave_rows<T>(config);
