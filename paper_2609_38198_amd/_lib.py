@@ -633,10 +633,16 @@ def _net_vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str
     return t.data_ptr()
 
 
-def _net_workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+def _net_workspace(ws: Optional[torch.Tensor], need: int, like: torch.Tensor) -> torch.Tensor:
     if ws is not None and ws.numel() * ws.element_size() >= need:
         return ws
-    return _workspace(need, device)
+    return like.new_empty(max(need, 1), dtype=torch.uint8)
+
+
+def _net_stream(device: torch.device) -> int:
+    # the current stream's handle without building a torch.cuda.Stream, which
+    # takes 2 us of a call's 12
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def fd_layer_norm(X: torch.Tensor, gamma: Optional[torch.Tensor] = None,
@@ -656,15 +662,15 @@ def fd_layer_norm(X: torch.Tensor, gamma: Optional[torch.Tensor] = None,
     pg = _net_vector(gamma, D, wdtype, "gamma")
     pb = _net_vector(beta, D, wdtype, "beta")
     if Y is None:
-        Y = torch.empty((N, D), dtype=X.dtype, device=X.device)
+        Y = X.new_empty((N, D))
     if stats is None:
-        stats = torch.empty((N, 2), dtype=torch.float32, device=X.device)
+        stats = X.new_empty((N, 2), dtype=torch.float32)
     _net_matrix(stats, N, 2, torch.float32, "stats")
     if not stats.is_contiguous():
         raise ValueError("stats must be contiguous")
     _check(lib.fd_layer_norm(X.data_ptr(), xt, N, D, ldx, pg, pb, wt, eps, Y.data_ptr(),
                              _net_matrix(Y, N, D, X.dtype, "Y"), stats.data_ptr(),
-                             _stream(X.device)))
+                             _net_stream(X.device)))
     return Y, stats
 
 
@@ -696,16 +702,16 @@ def fd_layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[to
     if not stats.is_contiguous():
         raise ValueError("stats must be contiguous")
     if dX is None:
-        dX = torch.empty((N, D), dtype=X.dtype, device=dev)
+        dX = X.new_empty((N, D))
     lddx = _net_matrix(dX, N, D, X.dtype, "dX")
-    dgamma = torch.empty(D, dtype=wdtype, device=dev) if weight_grads else None
-    dbeta = torch.empty(D, dtype=wdtype, device=dev) if weight_grads else None
-    ws = _net_workspace(ws, lib.fd_layer_norm_workspace_size(N, D), dev)
+    dgamma = X.new_empty(D, dtype=wdtype) if weight_grads else None
+    dbeta = X.new_empty(D, dtype=wdtype) if weight_grads else None
+    ws = _net_workspace(ws, lib.fd_layer_norm_workspace_size(N, D), X)
     _check(lib.fd_layer_norm_backward(
         dY.data_ptr(), lddy, X.data_ptr(), xt, N, D, ldx, pg, wt, stats.data_ptr(),
         None if add is None else add.data_ptr(), ldadd, dX.data_ptr(), lddx,
         dgamma.data_ptr() if weight_grads else None, dbeta.data_ptr() if weight_grads else None,
-        ws.data_ptr(), ws.numel() * ws.element_size(), _stream(dev)))
+        ws.data_ptr(), ws.numel() * ws.element_size(), _net_stream(dev)))
     return LayerNormGrads(dX, dgamma, dbeta)
 
 
@@ -741,18 +747,18 @@ def fd_gated_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: to
     b = _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act)
     dev = X.device
     if Y is None:
-        Y = torch.empty((b.N, b.O), dtype=X.dtype, device=dev)
+        Y = X.new_empty((b.N, b.O))
     ldy = _net_matrix(Y, b.N, b.O, X.dtype, "Y")
     ldr = 0 if R is None else _net_matrix(R, b.N, b.O, X.dtype, "R")
     saved, nsaved = None, 0
     if save:
         nsaved = lib.fd_gated_saved_size(b)
-        saved = _workspace(nsaved, dev)
+        saved = X.new_empty(max(nsaved, 1), dtype=torch.uint8)
     need = lib.fd_gated_workspace_size(b, 0)
-    ws = _net_workspace(ws, need, dev)
+    ws = _net_workspace(ws, need, X)
     _check(lib.fd_gated_forward(b, None if R is None else R.data_ptr(), ldr, Y.data_ptr(), ldy,
                                 saved.data_ptr() if save else None, nsaved, ws.data_ptr(),
-                                ws.numel() * ws.element_size(), _stream(dev)))
+                                ws.numel() * ws.element_size(), _net_stream(dev)))
     return Y, saved
 
 
@@ -781,7 +787,7 @@ def fd_gated_backward(dY: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: t
     lddy = _net_matrix(dY, b.N, b.O, t, "dY")
     if grads is None:
         def like(x):
-            return None if x is None else torch.empty(x.shape, dtype=t, device=dev)
+            return None if x is None else x.new_empty(x.shape)
 
         grads = GatedGrads(like(X) if want_dx else None, like(Wg), like(Wu), like(Wd), like(bg),
                            like(bu), like(bd))
@@ -796,10 +802,10 @@ def fd_gated_backward(dY: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: t
                     _net_matrix(g.dWd, b.O, b.F, t, "dWd"))
     nsaved = 0 if saved is None else saved.numel() * saved.element_size()
     need = lib.fd_gated_workspace_size(b, 2 if saved is None else 1)
-    ws = _net_workspace(ws, need, dev)
+    ws = _net_workspace(ws, need, X)
     _check(lib.fd_gated_backward(b, dY.data_ptr(), lddy,
                                  None if saved is None else saved.data_ptr(), nsaved, c,
-                                 ws.data_ptr(), ws.numel() * ws.element_size(), _stream(dev)))
+                                 ws.data_ptr(), ws.numel() * ws.element_size(), _net_stream(dev)))
     return grads
 
 
@@ -882,4 +888,4 @@ def fd_adamw_step(plan: AdamwPlan, step: int, lr: float = 1e-3, beta1: float = 0
                   grad_scale: float = 1.0) -> None:
     """One AdamW step over the plan's tensors, in place; `step` counts from 1."""
     o = AdamwOpts(lr, beta1, beta2, eps, weight_decay, grad_scale, step, plan.bits, 0)
-    _check(load().fd_adamw_step(plan.table, len(plan.table), o, _stream(plan.device)))
+    _check(load().fd_adamw_step(plan.table, len(plan.table), o, _net_stream(plan.device)))

@@ -5,6 +5,7 @@
 #include "fd_guard.hpp"
 #include "fd_solver.hpp"
 #include "net_gemm.hpp"
+#include "net_skinny.hpp"
 
 namespace fd {
 namespace net {
@@ -539,6 +540,14 @@ template <class T>
 void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void* Y, int64_t ldy,
              char* saved, hipStream_t st) {
   const int t = b.type;
+  if (b.N <= skinny_rows<T> && saved == nullptr) {
+    SkinnyArgs p{b.X, b.Wg, b.Wu, b.ldx, b.ldwi, b.N, b.F, b.D, b.bg, b.bu, nullptr, 0, w.h, b.F};
+    if (b.act == FD_ACT_SILU) launch_skinny<T, true, FD_ACT_SILU>(p, st);
+    else launch_skinny<T, true, FD_ACT_GELU>(p, st);
+    p = SkinnyArgs{w.h, b.Wd, nullptr, b.F, b.ldwd, b.N, b.O, b.F, b.bd, nullptr, R, ldr, Y, ldy};
+    launch_skinny<T, false, 0>(p, st);
+    return;
+  }
   const Matrix x = bring(w, b.X, b.ldx, b.N, b.D, t, w.x);
   Matrix wg, wu;
   bring_weights(w, b, wg, wu);

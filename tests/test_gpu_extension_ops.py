@@ -195,6 +195,22 @@ def test_gated_block_and_gradients(n, d, f, o, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("n, d, f, o", [(1, 3, 5, 2), (1, 1024, 700, 300), (2, 63, 64, 65),
+                                        (16, 500, 1030, 17), (17, 129, 48, 16), (33, 260, 515, 70),
+                                        (64, 96, 2050, 33), (65, 96, 205, 33)])
+def test_gated_few_rows_forward(n, d, f, o, pad, dtype):
+    act = "gelu" if n % 2 else "silu"
+    t, a = gated_inputs(n, d, f, o, dtype, d % 2 == 1, 31 * n + d, pad=pad)
+    case(f"gated few rows {n} x {d} -> {f} -> {o} {dtype} pad {pad}")
+    Y, _ = fd.fd_gated_forward(*[t[k] for k in ("X", "Wg", "Wu", "Wd", "bg", "bu", "bd")],
+                               R=t["R"], act=act)
+    want, _, _, H = ox.gated(a["X"], a["Wg"], a["Wu"], a["Wd"], a["bg"], a["bu"], a["bd"], a["R"],
+                             act)
+    assert err(Y, want, np.sqrt(((H ** 2) @ (a["Wd"] ** 2).T).sum())) <= GATED_TOL[dtype]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_gated_strides_recomputation_and_repeatability(dtype):
     # rows 3 elements further apart: nothing is 16-byte aligned
     t, a = gated_inputs(150, 64, 192, 40, dtype, True, 11, pad=3)
