@@ -54,7 +54,9 @@ def make(rng, shape, dtype, scale=1.0, mean=0.0, pad=0, offset=0):
 
 NORM_SHAPES = [(1, 1), (1, 8), (3, 2), (5, 3), (17, 30), (64, 64), (33, 127), (7, 129), (9, 301),
                (4099, 64), (257, 509), (130, 513), (65, 1000), (40, 1025), (21, 2047), (12, 2049),
-               (5, 4100), (3, 8200), (2, 16384), (2, 16385), (3, 20001)]
+               (5, 4100), (3, 8200), (2, 16384), (2, 16385), (3, 20001),
+               # many rows of less than a chunk, rows of one group of lanes less or more than whole
+               (3001, 3), (5000, 7), (300, 20000), (999, 61), (70, 259), (11, 5001)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
