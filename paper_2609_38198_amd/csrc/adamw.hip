@@ -66,41 +66,50 @@ __device__ __forceinline__ void update(const Step& s, float keep, float g, float
   p = p * keep - s.rate * m / (r * s.root + s.eps);
 }
 
-// Bound by memory: 28 bytes an element and 2 each for a bfloat16 gradient less
-// and a copy more; four elements of a lane are one 16-byte access of each array.
+// Bound by memory, 24 bytes an element and the gradient (28 in float32; 2 less and a
+// copy's 2 more in bfloat16).  Four elements of a lane are one 16-byte access of each array; a
+// lane asks for all its elements before it updates the first.
 __global__ __launch_bounds__(BLOCK) void adamw_kernel(Table tb, Step s) {
   const int ti = find_tensor(tb, blockIdx.x);
   const Tensor& t = tb.t[ti];
   const int64_t base = int64_t(blockIdx.x - tb.first[ti]) * CHUNK;
   float* M = static_cast<float*>(t.m);
   float* V = static_cast<float*>(t.v);
+  constexpr int EACH = CHUNK / (BLOCK * 4);
+  float p[EACH][4], g[EACH][4], m[EACH][4], v[EACH][4], r;
 #pragma unroll
-  for (int j = 0; j < CHUNK / (BLOCK * 4); ++j) {
+  for (int j = 0; j < EACH; ++j) {
     const int64_t at = base + (j * BLOCK + int(threadIdx.x)) * 4;
-    const int valid = int(min(int64_t(4), t.n - at));
-    if (valid <= 0) break;
-    float p[4], g[4], m[4], v[4], r;
-    load_wide<4>(t.p + at, valid, p);
-    load_grad(t, at, valid, g);
-    load_wide<4>(M + at, valid, m);
-    load_wide<4>(V + at, valid, v);
+    const int valid = int(max(int64_t(0), min(int64_t(4), t.n - at)));
+    load_wide<4>(t.p + at, valid, p[j]);
+    load_grad(t, at, valid, g[j]);
+    load_wide<4>(M + at, valid, m[j]);
+    load_wide<4>(V + at, valid, v[j]);
+  }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) update(s, t.keep, g[i], p[i], m[i], v[i], r);
-    store_wide<4>(t.p + at, valid, p);
-    store_wide<4>(M + at, valid, m);
-    store_wide<4>(V + at, valid, v);
-    if (t.copy != nullptr) store_wide<4>(t.copy + at, valid, p);
+  for (int j = 0; j < EACH; ++j) {
+    const int64_t at = base + (j * BLOCK + int(threadIdx.x)) * 4;
+    const int valid = int(max(int64_t(0), min(int64_t(4), t.n - at)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) update(s, t.keep, g[j][i], p[j][i], m[j][i], v[j][i], r);
+    store_wide<4>(t.p + at, valid, p[j]);
+    store_wide<4>(M + at, valid, m[j]);
+    store_wide<4>(V + at, valid, v[j]);
+    if (t.copy != nullptr) store_wide<4>(t.copy + at, valid, p[j]);
   }
 }
 
-__device__ __forceinline__ void widen_e4m3(const unsigned char* q, int valid, float scale,
-                                           float* out) {
+__device__ __forceinline__ int load_e4m3(const unsigned char* q, int valid) {
   int w = 0;
   if (valid >= 4) {
     __builtin_memcpy(&w, q, 4);
   } else {
     for (int i = 0; i < valid; ++i) w |= int(q[i]) << (8 * i);
   }
+  return w;
+}
+
+__device__ __forceinline__ void widen_e4m3(int w, float scale, float* out) {
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
   const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
   out[0] = lo[0] * scale;
@@ -141,7 +150,7 @@ __device__ __forceinline__ float narrow_e4m3(const float* x, unsigned char* q, i
 }
 
 // The 8-bit form: one wave takes the 256 elements that share a scale, so that
-// the new scale is a maximum over its lanes.  12 to 18 bytes an element.
+// the new scale is a maximum over its lanes.  12 bytes an element, the gradient and the copy.
 __global__ __launch_bounds__(BLOCK) void adamw_e4m3_kernel(Table tb, Step s) {
   const int ti = find_tensor(tb, blockIdx.x);
   const Tensor& t = tb.t[ti];
@@ -149,29 +158,41 @@ __global__ __launch_bounds__(BLOCK) void adamw_e4m3_kernel(Table tb, Step s) {
   unsigned char* M = static_cast<unsigned char*>(t.m);
   unsigned char* V = static_cast<unsigned char*>(t.v);
   const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
+  constexpr int EACH = CHUNK / (BLOCK * 4);
+  float p[EACH][4], g[EACH][4], ms[EACH], vs[EACH];
+  int qm[EACH], qv[EACH];
 #pragma unroll
-  for (int j = 0; j < CHUNK / (BLOCK * 4); ++j) {
+  for (int j = 0; j < EACH; ++j) {
+    const int64_t block = base + (j * (BLOCK / WAVE) + wave) * BLOCK, at = block + lane * 4;
+    const int valid = int(max(int64_t(0), min(int64_t(4), t.n - at)));
+    load_wide<4>(t.p + at, valid, p[j]);
+    load_grad(t, at, valid, g[j]);
+    qm[j] = load_e4m3(M + at, valid);
+    qv[j] = load_e4m3(V + at, valid);
+    ms[j] = block < t.n ? t.ms[block / BLOCK] : 0.f;
+    vs[j] = block < t.n ? t.vs[block / BLOCK] : 0.f;
+  }
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) {
     const int64_t block = base + (j * (BLOCK / WAVE) + wave) * BLOCK;
     if (block >= t.n) break;  // the whole wave
     const int64_t at = block + lane * 4;
     const int valid = int(max(int64_t(0), min(int64_t(4), t.n - at)));
-    float p[4], g[4], m[4], v[4], r[4];
-    load_wide<4>(t.p + at, valid, p);
-    load_grad(t, at, valid, g);
-    widen_e4m3(M + at, valid, t.ms[block / BLOCK], m);
-    widen_e4m3(V + at, valid, t.vs[block / BLOCK], r);
+    float m[4], v[4], r[4];
+    widen_e4m3(qm[j], ms[j], m);
+    widen_e4m3(qv[j], vs[j], r);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       v[i] = r[i] * r[i];
-      update(s, t.keep, g[i], p[i], m[i], v[i], r[i]);
+      update(s, t.keep, g[j][i], p[j][i], m[i], v[i], r[i]);
     }
-    store_wide<4>(t.p + at, valid, p);
-    if (t.copy != nullptr) store_wide<4>(t.copy + at, valid, p);
-    const float ms = narrow_e4m3<false>(m, M + at, valid);
-    const float vs = narrow_e4m3<true>(r, V + at, valid);
+    store_wide<4>(t.p + at, valid, p[j]);
+    if (t.copy != nullptr) store_wide<4>(t.copy + at, valid, p[j]);
+    const float m1 = narrow_e4m3<false>(m, M + at, valid);
+    const float r1 = narrow_e4m3<true>(r, V + at, valid);
     if (lane == 0) {
-      t.ms[block / BLOCK] = ms;
-      t.vs[block / BLOCK] = vs;
+      t.ms[block / BLOCK] = m1;
+      t.vs[block / BLOCK] = r1;
     }
   }
 }
