@@ -5,6 +5,7 @@
 #include "fd_guard.hpp"
 #include "fd_solver.hpp"
 #include "net_gemm.hpp"
+#include "net_narrow.hpp"
 #include "net_skinny.hpp"
 
 namespace fd {
@@ -402,6 +403,8 @@ Work carve_work_t(Arena& a, const fd_gated_block& b, int backward) {
     w.shapes[0] = shape_y<T>(b);
     w.config = plan<T>(w.shapes, 1, true, STORE, false);
     part = w.shapes[0].part();
+    if (b.D <= NARROW && b.O <= NARROW)
+      part = std::max(part, size_t(narrow_parts(b.N, b.F)) * size_t(b.N) * size_t(round_up(b.O, 4)));
   } else {
     w.dy = a.take<bf16>(packed<T>(b.N, b.O));
     w.dgu = a.take<bf16>(size_t(b.N) * 2 * Fp * planes_of<T>);
@@ -546,6 +549,17 @@ void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void*
     else launch_skinny<T, true, FD_ACT_GELU>(p, st);
     p = SkinnyArgs{w.h, b.Wd, nullptr, b.F, b.ldwd, b.N, b.O, b.F, b.bd, nullptr, R, ldr, Y, ldy};
     launch_skinny<T, false, 0>(p, st);
+    return;
+  }
+  if (b.D <= NARROW && b.O <= NARROW) {
+    NarrowArgs p{b, R, ldr, Y, ldy, saved, f_padded(b.F), narrow_parts(b.N, b.F), w.part, round_up(b.O, 4)};
+    run_narrow(p, st);
+    if (p.parts == 1) return;
+    AfterJobs after;
+    after.splits = 1;
+    after.s[0] = SplitJob{p.part, p.parts, b.N, b.O, p.ldp, {Y, nullptr}, ldy, b.N, b.N, b.bd, R, ldr, 0};
+    after.groups = ceil_div(b.N * ceil_div(b.O, 4), GROUP);
+    run_after<T>(after, st);
     return;
   }
   const Matrix x = bring(w, b.X, b.ldx, b.N, b.D, t, w.x);

@@ -161,15 +161,13 @@ struct Tile {
   }
 };
 
-// x as three bfloat16 values that add up to it; a value that is not finite is
-// the first one's alone.
+// x as three bfloat16 values that add up to it exactly: the first cut off (a
+// rounded one could leave the range), the others rounded.  An infinity becomes
+// a NaN.  Six instructions a value.
 __device__ __forceinline__ void split3(float x, bf16& a, bf16& b, bf16& c) {
-  a = bf16(x);
-  if (!(fabsf(float(a)) < INFINITY))  // rounded up past the largest, or not finite
-    a = __builtin_bit_cast(bf16, uint16_t(__builtin_bit_cast(uint32_t, x) >> 16 |
-                                          (x != x ? 0x40u : 0u)));
-  const float fa = float(a);
-  const float r = fabsf(fa) < INFINITY ? x - fa : 0.f;
+  const uint32_t top = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
+  a = __builtin_bit_cast(bf16, uint16_t(top >> 16));
+  const float r = x - __builtin_bit_cast(float, top);
   b = bf16(r);
   c = bf16(r - float(b));
 }
