@@ -162,9 +162,9 @@ __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
     __syncthreads();
     const Buffer& w = buf[cur];
     if (f0 + 32 < f_last) fetch(f0 + 32);
-    floatx16 g, u;
+    floatx16 g, u, gl, ul;  // low: the smaller plane pairs' sums
 #pragma unroll
-    for (int e = 0; e < 16; ++e) g[e] = u[e] = 0.f;
+    for (int e = 0; e < 16; ++e) g[e] = u[e] = gl[e] = ul[e] = 0.f;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       bf16x8 wg[PL], wu[PL];
@@ -175,11 +175,16 @@ __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
       }
 #pragma unroll
       for (int q = 0; q < PAIRS; ++q) {
-        g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wg[PL == 1 ? 0 : PB[q]], x[s][PL == 1 ? 0 : PA[q]], g, 0, 0, 0);
-        u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wu[PL == 1 ? 0 : PB[q]], x[s][PL == 1 ? 0 : PA[q]], u, 0, 0, 0);
+        floatx16 &tg = q + 1 == PAIRS ? g : gl, &tu = q + 1 == PAIRS ? u : ul;
+        tg = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wg[PL == 1 ? 0 : PB[q]], x[s][PL == 1 ? 0 : PA[q]], tg, 0, 0, 0);
+        tu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wu[PL == 1 ? 0 : PB[q]], x[s][PL == 1 ? 0 : PA[q]], tu, 0, 0, 0);
       }
     }
-    // last, as the tiles do: both make the same bits
+    if (PL > 1) {
+      g += gl;
+      u += ul;
+    }
+    // last, and all in the tiles' order: both make the same bits
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const floatx4 bg = *reinterpret_cast<const floatx4*>(&w.bias[0][8 * q + 4 * half]);

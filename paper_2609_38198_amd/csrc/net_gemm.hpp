@@ -416,13 +416,18 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
 
   const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
   const int wm = wave / WN, wn = wave % WN;
-  floatx16 acc[FM][FN];
+  // Three planes: the five smaller pairs have sums of their own, so that the
+  // large one is rounded once a k step and not six times.
+  floatx16 acc[FM][FN], low[PL == 1 ? 1 : FM][PL == 1 ? 1 : FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+      for (int e = 0; e < 16; ++e) {
+        acc[i][j][e] = 0.f;
+        if (PL > 1) low[i][j][e] = 0.f;
+      }
 
   // Fragments of k step ks of the tile in a buffer.  GATE: the first half of the n
   // fragments are gate columns, the others the same up columns.
@@ -452,9 +457,11 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
 #pragma unroll
       for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              fb[from][PL == 1 ? 0 : PB[q]][j], fa[from][PL == 1 ? 0 : PA[q]][i], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < FN; ++j) {
+          floatx16& to = q + 1 == PAIRS ? acc[i][j] : low[PL == 1 ? 0 : i][PL == 1 ? 0 : j];
+          to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              fb[from][PL == 1 ? 0 : PB[q]][j], fa[from][PL == 1 ? 0 : PA[q]][i], to, 0, 0, 0);
+        }
   };
   // The scheduler's order within a step: LDS reads evenly among the products.
   auto interleave = [] {
@@ -498,6 +505,12 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
       multiply(ks & 1);
       interleave();
     }
+  }
+  if (PL > 1) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] += low[PL == 1 ? 0 : i][PL == 1 ? 0 : j];
   }
   __syncthreads();  // the buffers become the waves' staging slabs
 
