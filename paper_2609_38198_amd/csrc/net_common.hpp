@@ -68,10 +68,18 @@ __device__ __forceinline__ float lane_sum(float x) {
   return x;
 }
 
+// Maximum over the wave, by data-parallel moves: within rows of 16 lanes, then
+// from row to row into lane 63.
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int d = WAVE / 2; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, WAVE));
-  return x;
+  auto step = [&](auto moved) { x = fmaxf(x, __builtin_bit_cast(float, moved)); };
+  const auto bits = [&] { return __builtin_bit_cast(int, x); };
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x111, 0xf, 0xf, false));  // row_shr:1
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x112, 0xf, 0xf, false));
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x114, 0xf, 0xf, false));
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x118, 0xf, 0xf, false));
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x142, 0xa, 0xf, false));  // row_bcast:15
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x143, 0xc, 0xf, false));  // row_bcast:31
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(bits(), WAVE - 1));
 }
 
 // Checks shared by the entry points.

@@ -285,24 +285,35 @@ __device__ __forceinline__ void save16(char* block, int which, int lane, const f
     *reinterpret_cast<float*>(block + which * 4) =
         __builtin_bit_cast(float, uint32_t(e - 14) << 23);
 }
+// The same, back: as it lies in memory (nothing waits for it yet), then widened.
 template <class T>
-__device__ __forceinline__ floatx16 saved16(const char* block, int which, int lane) {
+struct Kept {
+  floatx4 v[sizeof(T) == 4 ? 4 : 2];
+  float scale;
+};
+template <class T>
+__device__ __forceinline__ Kept<T> load_kept(const char* block, int which, int lane) {
+  Kept<T> k;
+  constexpr int N = sizeof(T) == 4 ? 4 : 2;
+  const char* p = block + (sizeof(T) == 4 ? which * 4096 : 16 + which * 2048);
+#pragma unroll
+  for (int q = 0; q < N; ++q) k.v[q] = *reinterpret_cast<const floatx4*>(p + (q * WAVE + lane) * 16);
+  k.scale = sizeof(T) == 4 ? 1.f : *reinterpret_cast<const float*>(block + which * 4);
+  return k;
+}
+template <class T>
+__device__ __forceinline__ floatx16 widen_kept(const Kept<T>& k) {
   floatx16 x;
-  if (sizeof(T) == 4) {
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const floatx4 v = *reinterpret_cast<const floatx4*>(block + which * 4096 + (q * WAVE + lane) * 16);
+    for (int i = 0; i < 16; ++i) x[i] = k.v[i / 4][i % 4];
+  } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * q + i] = v[i];
+    for (int q = 0; q < 2; ++q) {
+      const halfx8 v = __builtin_bit_cast(halfx8, k.v[q]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[8 * q + i] = float(v[i]) * k.scale;
     }
-    return x;
-  }
-  const float scale = *reinterpret_cast<const float*>(block + which * 4);
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const halfx8 v = *reinterpret_cast<const halfx8*>(block + 16 + which * 2048 + (q * WAVE + lane) * 16);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[8 * q + i] = float(v[i]) * scale;
   }
   return x;
 }
@@ -539,7 +550,7 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
       x[4 + i] = b[i];
     }
   };
-  const int64_t nw = n0 + wn * CN;          // the wave's first column
+  const int64_t nw = n0 + wn * CN;           // the wave's first column
   const int64_t nl = nw + (lane % LPR) * 8;  // the lane's, on reading back
 
   if (EPI == STORE && p.splits > 1) {
@@ -672,7 +683,7 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
         const int64_t fb = nw + j * 32;
         if (fb < p.Fp) {
           const char* block = saved_at<T>(p.saved, mb, fb, p.Fp);
-          const floatx16 g = saved16<T>(block, 0, lane), u = saved16<T>(block, 1, lane);
+          const floatx16 g = widen_kept(load_kept<T>(block, 0, lane)), u = widen_kept(load_kept<T>(block, 1, lane));
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const bool there = live && fb + 8 * (e / 4) + 4 * half32 + e % 4 < p.N;
