@@ -1,0 +1,163 @@
+"""A parametric extension of diffusion coordinates: a network x -> psi(x).
+
+The eigensolver gives the coordinates of the sampled points.  The Nystrom
+formula extends them to others, at the price of the whole sample for every
+batch; this program trains a small network on them instead, with the library's
+operators: a gated block D -> hidden -> width, `depth` residual ones on layer norms, one
+to the k coordinates, and AdamW.
+
+    python3 examples/extension_net.py [--dtype bf16] [--bits 8] [--points 65536]
+
+prints the training error, how far the network is from the Nystrom extension at
+new points, and how long each takes there.
+"""
+import argparse
+import math
+import os
+import sys
+import time
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2609_38198_amd import _lib as fd  # noqa: E402
+
+BLOCK = ("Wg", "Wu", "Wd", "bg", "bu", "bd")
+
+
+class ExtensionNet:
+    """Parameters are float32; with dtype bfloat16 the layers run on bfloat16
+    copies, which the optimizer's step writes."""
+
+    def __init__(self, d, k, width=64, hidden=256, depth=2, dtype=torch.float32, bits=32,
+                 act="silu", device="cuda", seed=0):
+        self.act, self.dtype = act, dtype
+        gen = torch.Generator().manual_seed(seed)
+        dims = [(d, width)] + [(width, width)] * depth + [(width, k)]
+        params, self.decay = [], []
+
+        def add(t, decay):
+            params.append(t.to(device=device, dtype=torch.float32).contiguous())
+            self.decay.append(decay)
+
+        for i, o in dims:
+            for shape in ((hidden, i), (hidden, i), (o, hidden)):
+                add(torch.randn(*shape, generator=gen) / math.sqrt(shape[1]), 1.0)
+            for size in (hidden, hidden, o):
+                add(torch.zeros(size), 0.0)
+        for _ in range(depth + 1):
+            add(torch.ones(width), 0.0)
+            add(torch.zeros(width), 0.0)
+        self.params = params
+        self.weights = params if dtype == torch.float32 else [p.to(dtype) for p in params]
+        self.grads = [torch.zeros_like(w) for w in self.weights]
+        self.state = fd.fd_adamw_state(params, bits)
+        self.plan = fd.fd_adamw_plan(params, self.grads, self.state, decay=self.decay,
+                                     copies=None if dtype == torch.float32 else self.weights)
+        self.layers, self.steps = len(dims), 0
+
+    def _block(self, tensors, i):
+        return tensors[6 * i:6 * i + 6]
+
+    def _norm(self, tensors, i):
+        at = 6 * self.layers + 2 * (i - 1)
+        return tensors[at], tensors[at + 1]
+
+    def forward(self, X, save=False):
+        """(Y, tape): the coordinates, and with save what backward needs."""
+        h, saved = fd.fd_gated_forward(X, *self._block(self.weights, 0), act=self.act, save=save)
+        tape = [(X, None, saved)]
+        for i in range(1, self.layers):
+            z, stats = fd.fd_layer_norm(h, *self._norm(self.weights, i))
+            inner = i + 1 < self.layers
+            y, saved = fd.fd_gated_forward(z, *self._block(self.weights, i), act=self.act,
+                                           save=save, R=h if inner else None)
+            tape.append((z, (h, stats), saved))
+            h = y
+        return h, tape
+
+    def backward(self, dY, tape):
+        """Fills self.grads."""
+        for i in reversed(range(self.layers)):
+            z, norm, saved = tape[i]
+            g = self._block(self.grads, i)
+            g = fd.GatedGrads(None if norm is None else torch.empty_like(z), *g)
+            fd.fd_gated_backward(dY, z, *self._block(self.weights, i), act=self.act, saved=saved,
+                                 grads=g)
+            if norm is None:
+                return
+            h, stats = norm
+            dgamma, dbeta = self._norm(self.grads, i)
+            dY = fd.fd_layer_norm_backward(
+                g.dX, h, self._norm(self.weights, i)[0], stats, dgamma=dgamma, dbeta=dbeta,
+                dX=g.dX, add=dY if i + 1 < self.layers else None).dX
+
+    def train_step(self, X, target, lr, weight_decay=1e-4):
+        """One step on mean squared error; the error, on the device."""
+        Y, tape = self.forward(X, save=True)
+        off = Y.float() - target
+        self.backward((off * (2.0 / off.numel())).to(self.dtype), tape)
+        self.steps += 1
+        fd.fd_adamw_step(self.plan, self.steps, lr=lr, weight_decay=weight_decay)
+        return off.square().mean()
+
+
+def torus(n, seed, device="cuda"):
+    t = torch.rand(n, 2, generator=torch.Generator().manual_seed(seed)) * (2.0 * math.pi)
+    return torch.stack([t[:, 0].cos(), t[:, 0].sin(), t[:, 1].cos(), t[:, 1].sin()], 1).to(device)
+
+
+def nystrom(new, X, beta, deg, psi, evals):
+    """psi(x) = K(x, X) (w psi) / (lambda K(x, X) w), w = q^-1/2."""
+    w = deg.q.rsqrt()[:, None]
+    Y = fd.fd_kernel_matmul(new, X, beta, torch.cat([w, w * psi], 1).contiguous())
+    return Y[:, 1:] / Y[:, :1] / evals
+
+
+def timed(f):
+    f()
+    torch.cuda.synchronize()
+    t = time.perf_counter()
+    for _ in range(20):
+        y = f()
+    torch.cuda.synchronize()
+    return y, (time.perf_counter() - t) / 20
+
+
+def main():
+    ap = argparse.ArgumentParser()
+    ap.add_argument("--dtype", choices=("f32", "bf16"), default="f32")
+    ap.add_argument("--bits", type=int, choices=(32, 8), default=32)
+    ap.add_argument("--points", type=int, default=16384)
+    ap.add_argument("--steps", type=int, default=400)
+    a = ap.parse_args()
+    n, k, beta, dtype = a.points, 5, 2.0, torch.float32 if a.dtype == "f32" else torch.bfloat16
+    both = torus(n + n // 4, 0)
+    X, new = both[:n].contiguous(), both[n:].contiguous()
+    # the first nontrivial coordinates: one group of four on this torus, fixed by
+    # the solve up to a rotation
+    eig = fd.fd_block_lanczos(X, beta, k, 8)
+    psi = eig.psi[:, 1:].contiguous()
+    scale = psi.square().mean().sqrt()
+    net = ExtensionNet(X.shape[1], k - 1, dtype=dtype, bits=a.bits)
+    target, inputs = psi / scale, X.to(dtype)
+    pick = torch.Generator(device="cuda").manual_seed(1)
+    for step in range(a.steps):
+        at = torch.randint(0, n, (4096,), device="cuda", generator=pick)
+        lr = 3e-3 * min(1.0, 4.0 * (1.0 - step / a.steps))
+        err = net.train_step(inputs[at], target[at], lr)
+        if step % 100 == 0 or step + 1 == a.steps:
+            print(f"step {step}: mean squared error {err.item():.2e}", flush=True)
+    evals = torch.tensor(eig.evals[1:], device="cuda", dtype=torch.float32)
+    deg = fd.fd_degree(X, beta)
+    y0, t0 = timed(lambda: nystrom(new, X, beta, deg, psi, evals))
+    points = new.to(dtype)
+    y1, t1 = timed(lambda: net.forward(points)[0])
+    off = (y1.float() * scale - y0).norm() / y0.norm()
+    print(f"{len(new)} new points: Nystrom {t0 * 1e6:.0f} us, network {t1 * 1e6:.0f} us, "
+          f"{off.item():.2e} apart")
+    return off.item()
+
+
+if __name__ == "__main__":
+    main()

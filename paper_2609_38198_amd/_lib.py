@@ -684,8 +684,11 @@ class LayerNormGrads:
 def fd_layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[torch.Tensor],
                            stats: torch.Tensor, add: Optional[torch.Tensor] = None,
                            weight_grads: bool = True, dX: Optional[torch.Tensor] = None,
+                           dgamma: Optional[torch.Tensor] = None,
+                           dbeta: Optional[torch.Tensor] = None,
                            ws: Optional[torch.Tensor] = None) -> LayerNormGrads:
-    """Gradients of fd_layer_norm; `add`, a residual branch's gradient, is added to dX."""
+    """Gradients of fd_layer_norm, into dX, dgamma and dbeta where given; `add`, a
+    residual branch's gradient, is added to dX."""
     lib = load()
     if X.dim() != 2:
         raise ValueError("X must be N x D")
@@ -704,14 +707,16 @@ def fd_layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[to
     if dX is None:
         dX = X.new_empty((N, D))
     lddx = _net_matrix(dX, N, D, X.dtype, "dX")
-    dgamma = X.new_empty(D, dtype=wdtype) if weight_grads else None
-    dbeta = X.new_empty(D, dtype=wdtype) if weight_grads else None
+    if weight_grads:
+        dgamma = X.new_empty(D, dtype=wdtype) if dgamma is None else dgamma
+        dbeta = X.new_empty(D, dtype=wdtype) if dbeta is None else dbeta
+    pdg = _net_vector(dgamma, D, wdtype, "dgamma")
+    pdb = _net_vector(dbeta, D, wdtype, "dbeta")
     ws = _net_workspace(ws, lib.fd_layer_norm_workspace_size(N, D), X)
     _check(lib.fd_layer_norm_backward(
         dY.data_ptr(), lddy, X.data_ptr(), xt, N, D, ldx, pg, wt, stats.data_ptr(),
         None if add is None else add.data_ptr(), ldadd, dX.data_ptr(), lddx,
-        dgamma.data_ptr() if weight_grads else None, dbeta.data_ptr() if weight_grads else None,
-        ws.data_ptr(), ws.numel() * ws.element_size(), _net_stream(dev)))
+        pdg, pdb, ws.data_ptr(), ws.numel() * ws.element_size(), _net_stream(dev)))
     return LayerNormGrads(dX, dgamma, dbeta)
 
 
