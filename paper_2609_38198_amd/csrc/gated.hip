@@ -236,9 +236,10 @@ int plan(Shape* s, int count, bool split, int epilogue, bool columns) {
       k[i] = double(s[i].ktiles);
       mn[i] = double(s[i].M) * double(s[i].N);
     }
-    for (int cap = split ? 4 : 1024; cap <= 1024; cap *= 2) {
+    const bool may = split && (epilogue == STORE || c != BIG);
+    for (int cap = may ? 4 : 1024; cap <= 1024; cap *= 2) {
       // of the products longer than the cap, those in the mask are split
-      for (int mask = 0; mask < (split ? 1 << count : 1); ++mask) {
+      for (int mask = 0; mask < (may ? 1 << count : 1); ++mask) {
         double groups = 0, work = 0, longest = 0, sums = 0;
         int n[GROUP_GEMMS];
         bool fresh = true;
@@ -257,7 +258,7 @@ int plan(Shape* s, int count, bool split, int epilogue, bool columns) {
         if (!fresh) continue;
         const double rounds = groups / double(CUS);
         const double time = std::max(work / double(CUS) * std::ceil(rounds) / std::max(rounds, 1e-9), longest) +
-                            (sums > 0 ? sums + 4.0 : 0.0);
+                            (sums > 0 ? sums + (epilogue == STORE ? 4.0 : 8.0) : 0.0);
         if (time < best) {
           best = time;
           config = c;
@@ -299,6 +300,19 @@ void launch(int config, GemmArgs& p, hipStream_t stream) {
   if (config == BIG) launch_config<BIG, ACOL, BCOL, EPI, T, ACT>(p, stream);
   else if (config == MID) launch_config<MID, ACOL, BCOL, EPI, T, ACT>(p, stream);
   else launch_config<SMALL, ACOL, BCOL, EPI, T, ACT>(p, stream);
+}
+
+// GATE or GRAD in the tile and parts of a plan, and the rest where there are parts.
+template <bool BCOL, int EPI, class T, int ACT>
+void launch_inner(int config, const Shape& s, float* part, GemmArgs& p, hipStream_t stream) {
+  p.splits = s.splits;
+  p.part = part;
+  launch<false, BCOL, EPI, T, ACT>(config, p, stream);
+  if (s.splits == 1) return;
+  const int64_t groups = ceil_div(ceil_div(p.M, 32) * (p.Fp / 32), GROUP / WAVE);
+  check_grid(groups);
+  finish_kernel<EPI, T, ACT><<<dim3(unsigned(groups)), dim3(GROUP), 0, stream>>>(p);
+  FD_LAUNCH_CHECK();
 }
 
 template <int C, class T>
@@ -357,6 +371,9 @@ struct Work {
   // the forward pass's Y, or the backward pass's dX, [dWg; dWu], dWd
   Shape shapes[GROUP_GEMMS];
   int config = SMALL;
+  // G and U; dH
+  Shape gate, grad;
+  int gate_config = SMALL, grad_config = SMALL;
 };
 
 int64_t f_padded(int64_t F) { return round_up(F, F_PAD); }
@@ -397,23 +414,34 @@ Work carve_work_t(Arena& a, const fd_gated_block& b, int backward) {
   w.wu = a.take<bf16>(packed<T>(b.F, b.D));
   w.wd = a.take<bf16>(packed<T>(b.O, b.F));
   const int64_t Fp = f_padded(b.F);
+  const size_t blocks = size_t(ceil_div(b.N, 32)) * size_t(Fp / 32);
   w.h = a.take<bf16>(size_t(b.N) * Fp * planes_of<T>);
   size_t part = 0;
+  if (backward != 1) {
+    w.gate = Shape{b.N, 2 * b.F, ceil_div(b.D, k_tile<T>)};
+    w.gate_config = plan<T>(&w.gate, 1, true, GATE, false);
+    if (w.gate.splits > 1) part = size_t(w.gate.splits) * blocks * 2048;
+  }
   if (backward == 0) {
     w.shapes[0] = shape_y<T>(b);
     w.config = plan<T>(w.shapes, 1, true, STORE, false);
-    part = w.shapes[0].part();
+    part = std::max(part, w.shapes[0].part());
     if (b.D <= NARROW && b.O <= NARROW)
       part = std::max(part, size_t(narrow_parts(b.N, b.F)) * size_t(b.N) * size_t(round_up(b.O, 4)));
   } else {
     w.dy = a.take<bf16>(packed<T>(b.N, b.O));
     w.dgu = a.take<bf16>(size_t(b.N) * 2 * Fp * planes_of<T>);
-    // tiles of 64 or 128 rows have two rows of waves, of 256 rows at most four
+    // a row for each 32 rows, or each row of waves of a tile: tiles of 64 or 128
+    // rows have two, of 256 rows at most four
     w.colsum = a.take<float>(size_t(2 * ceil_div(b.N, 64) + 2) * 2 * Fp);
     w.dysum = a.take<float>(size_t(SUM_PARTS) * size_t(b.O));
     shapes_grad<T>(b, w.shapes);
     w.config = plan<T>(w.shapes, GROUP_GEMMS, true, STORE, true);
-    for (const Shape& s : w.shapes) part += s.part();
+    size_t sum = 0;
+    for (const Shape& s : w.shapes) sum += s.part();
+    w.grad = Shape{b.N, b.F, ceil_div(b.O, k_tile<T>)};
+    w.grad_config = plan<T>(&w.grad, 1, true, GRAD, true);
+    part = std::max({part, sum, w.grad.splits > 1 ? size_t(w.grad.splits) * blocks * 1024 : 0});
     if (backward == 2) w.saved = a.take<char>(saved_bytes(b));
   }
   w.part = a.take<float>(part);
@@ -470,7 +498,7 @@ void run_gate(const fd_gated_block& b, const Work& w, const Matrix& x, const Mat
   p.up = wu.p;
   p.M = b.N;
   p.N = b.F;
-  p.segs = p.splits = 1;
+  p.segs = 1;
   p.ktiles = ceil_div(x.cols, k_tile<T>);
   p.bg = b.bg;
   p.bu = b.bu;
@@ -478,10 +506,8 @@ void run_gate(const fd_gated_block& b, const Work& w, const Matrix& x, const Mat
   p.Fp = f_padded(b.F);
   p.H = h ? w.h : nullptr;
   p.hplane = b.N * p.Fp;
-  Shape s{b.N, 2 * b.F, p.ktiles};
-  const int config = plan<T>(&s, 1, false, GATE, false);
-  if (b.act == FD_ACT_SILU) launch<false, false, GATE, T, FD_ACT_SILU>(config, p, st);
-  else launch<false, false, GATE, T, FD_ACT_GELU>(config, p, st);
+  if (b.act == FD_ACT_SILU) launch_inner<false, GATE, T, FD_ACT_SILU>(w.gate_config, w.gate, w.part, p, st);
+  else launch_inner<false, GATE, T, FD_ACT_GELU>(w.gate_config, w.gate, w.part, p, st);
 }
 
 void check_block(const fd_gated_block* bp) {
@@ -645,7 +671,7 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
     p.b = columns_of(wd);
     p.M = b.N;
     p.N = b.F;
-    p.segs = p.splits = 1;
+    p.segs = 1;
     p.ktiles = ceil_div(b.O, k_tile<T>);
     p.saved = saved;
     p.Fp = Fp;
@@ -654,11 +680,9 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
     p.dGU = w.dgu;
     p.gplane = b.N * 2 * Fp;
     p.colsum = g.dbg != nullptr || g.dbu != nullptr ? w.colsum : nullptr;
-    Shape s{b.N, b.F, p.ktiles};
-    const int config = plan<T>(&s, 1, false, GRAD, true);
-    if (b.act == FD_ACT_SILU) launch<false, true, GRAD, T, FD_ACT_SILU>(config, p, st);
-    else launch<false, true, GRAD, T, FD_ACT_GELU>(config, p, st);
-    const int64_t wave_rows = p.tiles_m * grad_wave_rows<T>(config);
+    if (b.act == FD_ACT_SILU) launch_inner<true, GRAD, T, FD_ACT_SILU>(w.grad_config, w.grad, w.part, p, st);
+    else launch_inner<true, GRAD, T, FD_ACT_GELU>(w.grad_config, w.grad, w.part, p, st);
+    const int64_t sum_rows = w.grad.splits > 1 ? ceil_div(b.N, 32) : p.tiles_m * grad_wave_rows<T>(w.grad_config);
 
     const Matrix h{w.h, Fp, b.N, Fp, b.N * Fp}, dgu{w.dgu, 2 * Fp, b.N, 2 * Fp, b.N * 2 * Fp};
     Shape shapes[GROUP_GEMMS];
@@ -714,7 +738,7 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
       else launch_group<SMALL, T>(group, st);
     }
     if (g.dbg != nullptr || g.dbu != nullptr)
-      add_columns(after, w.colsum, wave_rows, 2 * Fp, Fp, b.F, g.dbg, g.dbu);
+      add_columns(after, w.colsum, sum_rows, 2 * Fp, Fp, b.F, g.dbg, g.dbu);
   }
   if (g.dbd != nullptr) add_columns(after, w.dysum, parts, b.O, b.O, b.O, g.dbd, nullptr);
   run_after<T>(after, st);

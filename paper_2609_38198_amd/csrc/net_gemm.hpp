@@ -230,7 +230,8 @@ struct GemmArgs {
   int64_t ldr;
   float* part;
   int64_t ldp;
-  // GATE, GRAD
+  // GATE, GRAD; where k is split, the blocks' raw accumulators go to part, by
+  // part and block as the kept ones lie in float32, and a kernel after it does the rest
   const void *bg, *bu;  // of the block's type, or NULL
   char* saved;          // G and U by 32 x 32 blocks, or NULL
   int64_t Fp;           // F rounded up to F_PAD: the planes' row length
@@ -615,6 +616,25 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
     }
   };
 
+  // (not of the largest tiles, whose epilogues have no register to spare)
+  if (EPI != STORE && BM < 256 && p.splits > 1) {
+    constexpr int MATS = EPI == GATE ? 2 : 1, HALF = FN / MATS > 0 ? FN / MATS : 1;
+    const int64_t blocks = (p.M + 31) / 32 * (p.Fp / 32);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int64_t mb = m0 + wm * TM + i * 32;
+      if (mb >= p.M) break;
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const int64_t fb = nw + j % HALF * 32;
+        if (fb >= p.Fp) continue;
+        const int64_t block = split * blocks + mb / 32 * (p.Fp / 32) + fb / 32;
+        save16<float>(reinterpret_cast<char*>(p.part + block * (MATS * 1024)), j / HALF, lane, acc[i][j]);
+      }
+    }
+    return;
+  }
+
   if (EPI == GATE) {
     constexpr int HALF = FN / 2 > 0 ? FN / 2 : 1;
 #pragma unroll
@@ -752,6 +772,98 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_group_kernel(GemmGroup s)
     gemm_body<BM, BN, WM, WN, true, true, STORE, T, 0>(s.g[i], id, smem);
   else
     gemm_body<BM, BN, WM, WN, false, true, STORE, T, 0>(s.g[i], id, smem);
+}
+
+// The rest of a GATE or GRAD product whose k is split: a wave to a 32 x 32 block
+// adds the parts in their order and goes on as the product's own epilogue does.
+template <int EPI, class T, int ACT>
+__global__ __launch_bounds__(256) void finish_kernel(GemmArgs p) {
+  constexpr int MATS = EPI == GATE ? 2 : 1;
+  const int lane = threadIdx.x % WAVE, half32 = lane / 32;
+  const int64_t across = p.Fp / 32, blocks = (p.M + 31) / 32 * across;
+  const int64_t at = int64_t(blockIdx.x) * (256 / WAVE) + threadIdx.x / WAVE;
+  if (at >= blocks) return;
+  const int64_t mb = at / across * 32, fb = at % across * 32, m = mb + lane % 32;
+  floatx16 x[2];
+#pragma unroll
+  for (int w = 0; w < MATS; ++w) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[w][e] = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s)
+      x[w] += widen_kept(load_kept<float>(
+          reinterpret_cast<const char*>(p.part + (s * blocks + at) * (MATS * 1024)), w, lane));
+  }
+  floatx16 out[3];
+  if (EPI == GATE) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t f = fb + 8 * q + 4 * half32;
+      const int valid = int(max(int64_t(0), min(int64_t(4), p.N - f)));
+      float bg[4] = {0.f, 0.f, 0.f, 0.f}, bu[4] = {0.f, 0.f, 0.f, 0.f};
+      if (p.bg != nullptr) load_wide<4>(static_cast<const T*>(p.bg) + f, valid, bg);
+      if (p.bu != nullptr) load_wide<4>(static_cast<const T*>(p.bu) + f, valid, bu);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = 4 * q + e;
+        x[0][i] += bg[e];
+        x[1][i] += bu[e];
+        out[2][i] = e < valid ? activate<ACT>(x[0][i]).value * x[1][i] : 0.f;
+      }
+    }
+    if (p.saved != nullptr) {
+      char* block = saved_at<T>(p.saved, mb, fb, p.Fp);
+      save16<T>(block, 0, lane, x[0]);
+      save16<T>(block, 1, lane, x[1]);
+    }
+  } else {
+    const char* block = saved_at<T>(p.saved, mb, fb, p.Fp);
+    const floatx16 g = widen_kept(load_kept<T>(block, 0, lane)), u = widen_kept(load_kept<T>(block, 1, lane));
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int64_t f = fb + 8 * (e / 4) + 4 * half32 + e % 4;
+      const bool there = m < p.M && f < p.N;
+      const Act a = activate<ACT>(g[e]);
+      const float dh = x[0][e];
+      out[0][e] = there ? dh * u[e] * a.slope : 0.f;
+      out[1][e] = there ? dh * a.value : 0.f;
+      out[2][e] = there ? a.value * u[e] : 0.f;
+      if (p.colsum != nullptr) {  // a row of sums for each 32 rows
+        const float sg = lane_sum<32>(out[0][e]), su = lane_sum<32>(out[1][e]);
+        if (lane % 32 == 0) {
+          p.colsum[mb / 32 * 2 * p.Fp + f] = sg;
+          p.colsum[mb / 32 * 2 * p.Fp + p.Fp + f] = su;
+        }
+      }
+    }
+  }
+  if (m >= p.M) return;
+#pragma unroll
+  for (int w = EPI == GATE ? 2 : 0; w < 3; ++w) {
+    if (w == 2 && p.H == nullptr) continue;
+    bf16* to = w == 2 ? p.H + m * p.Fp : p.dGU + m * 2 * p.Fp + w * p.Fp;
+    const int64_t plane = w == 2 ? p.hplane : p.gplane;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      bf16x4 v[3];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float y = out[w][4 * q + e];
+        if (sizeof(T) == 4) {
+          bf16 a, b, c;
+          split3(y, a, b, c);
+          v[0][e] = a;
+          v[1][e] = b;
+          v[2][e] = c;
+        } else {
+          v[0][e] = bf16(y);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < planes_of<T>; ++k)
+        *reinterpret_cast<bf16x4*>(to + k * plane + fb + 8 * q + 4 * half32) = v[k];
+    }
+  }
 }
 
 }  // namespace net

@@ -141,6 +141,8 @@ GATED_SHAPES = [(1, 1, 1, 1), (1, 4, 16, 4), (1, 1024, 512, 256), (2, 30, 97, 64
                 (127, 130, 191, 66), (129, 128, 128, 128), (200, 8, 24, 16), (257, 509, 333, 509),
                 (1000, 30, 512, 64), (2049, 96, 160, 72), (3000, 16, 40, 8),
                 # every tile of each product: many rows, wide inner, wide outer sides
+                # few tiles and long sums over D and O
+                (70, 2000, 90, 1500), (336, 1696, 372, 700),
                 (33000, 7, 70, 33), (501, 33, 31, 64), (4100, 24, 2100, 16), (4104, 4100, 40, 4098), (700, 40, 4099, 2050)]
 
 
