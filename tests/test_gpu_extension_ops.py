@@ -226,6 +226,27 @@ def test_gated_strides_recomputation_and_repeatability(dtype):
         assert torch.equal(getattr(g1, name), getattr(g2, name)), name
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gated_single_gradients(dtype):
+    # each gradient alone, the others NULL: the same bits, and nothing else is needed
+    t, a = gated_inputs(300, 72, 130, 90, dtype, True, 17)
+    w = [t[k] for k in ("X", "Wg", "Wu", "Wd", "bg", "bu", "bd")]
+    case(f"gated single gradients {dtype}")
+    full = fd.fd_gated_backward(t["dY"], *w)
+    lib = fd.load()
+    b = fd._gated_block(*w, "silu")
+    ws = torch.empty(lib.fd_gated_workspace_size(b, 2), dtype=torch.uint8, device=device())
+    stream = torch.cuda.current_stream().cuda_stream
+    for name in ("dX", "dWg", "dWu", "dWd", "dbg", "dbu", "dbd"):
+        want = getattr(full, name)
+        got = torch.full_like(want, float("nan"))
+        g = fd.GatedGradsC(lddx=72, lddwi=72, lddwd=130)
+        setattr(g, name, got.data_ptr())
+        assert lib.fd_gated_backward(b, t["dY"].data_ptr(), 90, None, 0, g, ws.data_ptr(),
+                                     ws.numel(), stream) == 0
+        assert torch.equal(got, want), name
+
+
 def test_gated_gradients_against_differences():
     # float64 differences of the oracle's own forward: the formulas themselves
     t, a = gated_inputs(6, 5, 9, 4, F32, True, 12)
