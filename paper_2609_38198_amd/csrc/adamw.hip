@@ -11,7 +11,6 @@ namespace {
 
 constexpr int BLOCK = 256;      // elements that share a scale, and threads of a workgroup
 constexpr int CHUNK = 4096;     // elements of a workgroup
-constexpr int TABLE = 48;       // tensors of a launch: the table travels in its arguments (4 KB at most)
 constexpr float E4M3_TOP = 448.f;
 constexpr float E4M3_LEAST = 0x1p-9f;
 constexpr float LEAST_TOP = 0x1p-100f;  // a block below this is stored as zeros
@@ -21,23 +20,33 @@ struct Tensor {
   const void* g;
   void* m;
   void* v;
-  float *ms, *vs;
   bf16* copy;
   int64_t n;
   int32_t gt;
   float keep;      // 1 - lr wd
 };
-struct Table {
-  Tensor t[TABLE];
-  uint32_t first[TABLE + 1];  // a tensor's first workgroup
-  int32_t count;
+struct ScaledTensor : Tensor {  // of 8-bit states
+  float *ms, *vs;
 };
 struct Step {
   float b1, nb1, b2, nb2, rate, root, eps, gscale;
 };
+// The tensors of a launch travel in its arguments, of which there are 4 KB: a launch
+// less is 5 to 7 us of a step (60 tensors, 14.9 million elements: 100 us in two, 92 in one).
+template <class E, int COUNT>
+struct Table {
+  E t[COUNT];
+  uint32_t first[COUNT + 1];  // a tensor's first workgroup
+  int32_t count = 0;
+};
+using PlainTable = Table<Tensor, 64>;
+using ScaledTable = Table<ScaledTensor, 48>;
+static_assert(sizeof(PlainTable) + sizeof(Step) <= 4096 && sizeof(ScaledTable) + sizeof(Step) <= 4096,
+              "a launch's arguments");
 
 // The tensor of a workgroup: the last one whose first workgroup is not after it.
-__device__ __forceinline__ int find_tensor(const Table& tb, uint32_t wg) {
+template <class TB>
+__device__ __forceinline__ int find_tensor(const TB& tb, uint32_t wg) {
   int lo = 0, hi = tb.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
@@ -68,8 +77,8 @@ __device__ __forceinline__ void update(const Step& s, float keep, float g, float
 
 // Bound by memory, 24 bytes an element and the gradient (28 in float32; 2 less and a
 // copy's 2 more in bfloat16).  Four elements of a lane are one 16-byte access of each array; a
-// lane asks for all its elements before it updates the first.
-__global__ __launch_bounds__(BLOCK) void adamw_kernel(Table tb, Step s) {
+// lane asks for all its elements before it updates the first (14.9 million elements: 92 us, 107 without, 4.5 TB/s).
+__global__ __launch_bounds__(BLOCK) void adamw_kernel(PlainTable tb, Step s) {
   const int ti = find_tensor(tb, blockIdx.x);
   const Tensor& t = tb.t[ti];
   const int64_t base = int64_t(blockIdx.x - tb.first[ti]) * CHUNK;
@@ -150,10 +159,11 @@ __device__ __forceinline__ float narrow_e4m3(const float* x, unsigned char* q, i
 }
 
 // The 8-bit form: one wave takes the 256 elements that share a scale, so that
-// the new scale is a maximum over its lanes.  12 bytes an element, the gradient and the copy.
-__global__ __launch_bounds__(BLOCK) void adamw_e4m3_kernel(Table tb, Step s) {
+// the new scale is a maximum over its lanes.  12 bytes an element, the gradient and the copy:
+// 152 million elements in 474 us, 5.1 TB/s.
+__global__ __launch_bounds__(BLOCK) void adamw_e4m3_kernel(ScaledTable tb, Step s) {
   const int ti = find_tensor(tb, blockIdx.x);
-  const Tensor& t = tb.t[ti];
+  const ScaledTensor& t = tb.t[ti];
   const int64_t base = int64_t(blockIdx.x - tb.first[ti]) * CHUNK;
   unsigned char* M = static_cast<unsigned char*>(t.m);
   unsigned char* V = static_cast<unsigned char*>(t.v);
@@ -195,6 +205,50 @@ __global__ __launch_bounds__(BLOCK) void adamw_e4m3_kernel(Table tb, Step s) {
       t.vs[block / BLOCK] = r1;
     }
   }
+}
+
+void set_scales(Tensor&, const fd_adamw_tensor&) {}
+void set_scales(ScaledTensor& d, const fd_adamw_tensor& t) {
+  d.ms = t.m_scale;
+  d.vs = t.v_scale;
+}
+
+// A launch for each table of tensors, or 2^30 workgroups.
+template <class TB>
+void run(void (*kernel)(TB, Step), const fd_adamw_tensor* tensors, int64_t count,
+         const fd_adamw_opts& o, const Step& s, hipStream_t st) {
+  constexpr int64_t MAX_GROUPS = int64_t(1) << 30;
+  constexpr int ROOM = int(sizeof(TB::t) / sizeof(TB::t[0]));
+  TB tb{};
+  int64_t groups = 0;
+  auto flush = [&] {
+    if (tb.count == 0) return;
+    tb.first[tb.count] = uint32_t(groups);
+    kernel<<<dim3(unsigned(groups)), dim3(BLOCK), 0, st>>>(tb, s);
+    FD_LAUNCH_CHECK();
+    tb.count = 0;
+    groups = 0;
+  };
+  for (int64_t i = 0; i < count; ++i) {
+    const fd_adamw_tensor& t = tensors[i];
+    if (t.n == 0) continue;
+    const int64_t need = ceil_div(t.n, CHUNK);
+    if (tb.count == ROOM || groups + need > MAX_GROUPS) flush();
+    auto& d = tb.t[tb.count];
+    d.p = t.p;
+    d.g = t.g;
+    d.m = t.m;
+    d.v = t.v;
+    d.copy = static_cast<bf16*>(t.copy);
+    d.n = t.n;
+    d.gt = t.gt;
+    d.keep = float(1.0 - o.lr * o.weight_decay * double(t.decay));
+    set_scales(d, t);
+    tb.first[tb.count] = uint32_t(groups);
+    ++tb.count;
+    groups += need;
+  }
+  flush();
 }
 
 }  // namespace
@@ -262,34 +316,10 @@ fd_status fd_adamw_step(const fd_adamw_tensor* tensors, int64_t count, const fd_
     s.eps = float(o.eps);
     s.gscale = float(o.grad_scale);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    // a launch takes TABLE tensors and 2^30 workgroups at most
-    constexpr int64_t MAX_GROUPS = int64_t(1) << 30;
-    Table tb{};
-    int64_t groups = 0;
-    auto flush = [&] {
-      if (tb.count == 0) return;
-      tb.first[tb.count] = uint32_t(groups);
-      if (narrow_states)
-        adamw_e4m3_kernel<<<dim3(unsigned(groups)), dim3(BLOCK), 0, st>>>(tb, s);
-      else
-        adamw_kernel<<<dim3(unsigned(groups)), dim3(BLOCK), 0, st>>>(tb, s);
-      FD_LAUNCH_CHECK();
-      tb.count = 0;
-      groups = 0;
-    };
-    for (int64_t i = 0; i < count; ++i) {
-      const fd_adamw_tensor& t = tensors[i];
-      if (t.n == 0) continue;
-      const int64_t need = ceil_div(t.n, CHUNK);
-      if (tb.count == TABLE || groups + need > MAX_GROUPS) flush();
-      Tensor& d = tb.t[tb.count];
-      d = Tensor{t.p,       t.g,       t.m, t.v, t.m_scale, t.v_scale, static_cast<bf16*>(t.copy),
-                 t.n, t.gt, float(1.0 - o.lr * o.weight_decay * double(t.decay))};
-      tb.first[tb.count] = uint32_t(groups);
-      ++tb.count;
-      groups += need;
-    }
-    flush();
+    if (narrow_states)
+      run<ScaledTable>(adamw_e4m3_kernel, tensors, count, o, s, st);
+    else
+      run<PlainTable>(adamw_kernel, tensors, count, o, s, st);
   });
 }
 

