@@ -78,7 +78,7 @@ __global__ __launch_bounds__(GROUP) void before_kernel(PackJobs jobs) {
   float x[8];
   load_wide<8>(static_cast<const T*>(job.src) + row * job.ld + col,
                int(min(int64_t(8), job.cols - col)), x);
-  write_planes<T>(job.dst + row * job.ldp + col, job.plane, x);
+  write_planes<planes_of<T>>(job.dst + row * job.ldp + col, job.plane, x);
 }
 
 // ---------------------------------------------------------------- after
@@ -230,16 +230,16 @@ struct Shape {
   size_t part() const { return splits == 1 ? 0 : size_t(splits) * size_t(M) * size_t(round_up(N, 4)); }
 };
 
-// The tile, and the parts of each product's k (with `split`), of a launch of
+// The tile (the smallest with `fine`), and the parts of each product's k, of a launch of
 // `count` products: the least of an estimate that counts whole rounds of a
 // workgroup a CU, the longest workgroup, and the traffic of the parts' sums.
 template <class T>
-int plan(Shape* s, int count, bool split, int epilogue, bool columns) {
+int plan(Shape* s, int count, bool fine, int epilogue, bool columns) {
   const TileCost* costs = tile_costs<T>();
   double best = 1e30;
   int config = SMALL;
   int parts[GROUP_GEMMS] = {1, 1, 1};
-  for (int c = 0; c < CONFIGS; ++c) {
+  for (int c = fine ? SMALL : BIG; c < CONFIGS; ++c) {
     const TileCost& t = costs[c];
     const double rest = t.rest[epilogue];
     double tiles[GROUP_GEMMS], k[GROUP_GEMMS], mn[GROUP_GEMMS];
@@ -248,7 +248,7 @@ int plan(Shape* s, int count, bool split, int epilogue, bool columns) {
       k[i] = double(s[i].ktiles);
       mn[i] = double(s[i].M) * double(s[i].N);
     }
-    const bool may = split && (epilogue == STORE || c != BIG);
+    const bool may = epilogue == STORE || c != BIG;
     for (int cap = may ? 4 : 1024; cap <= 1024; cap *= 2) {
       // of the products longer than the cap, those in the mask are split
       for (int mask = 0; mask < (may ? 1 << count : 1); ++mask) {
@@ -294,14 +294,15 @@ void allow_lds(K kernel, size_t bytes) {
                                    hipFuncAttributeMaxDynamicSharedMemorySize, int(bytes)));
 }
 
-template <int C, bool ACOL, bool BCOL, int EPI, class T, int ACT>
+template <int C, bool ACOL, bool BCOL, int EPI, class T, int ACT, int HP>
 void launch_config(GemmArgs& p, hipStream_t stream) {
   using K = Config<C, EPI, T>;
-  constexpr size_t lds = gemm_lds<K::bm, K::bn, K::wm, K::wn, T>;
+  constexpr int PL = planes_of<T>, PLA = EPI == STORE ? HP : PL;
+  constexpr size_t lds = gemm_lds<K::bm, K::bn, T, PLA, PL>;
   p.tiles_m = ceil_div(p.M, K::bm);
   // GATE and GRAD write whole padded rows
   p.tiles_n = ceil_div(EPI == STORE ? p.N : p.Fp, EPI == GATE ? K::bn / 2 : K::bn);
-  auto kernel = gemm_kernel<K::bm, K::bn, K::wm, K::wn, ACOL, BCOL, EPI, T, ACT>;
+  auto kernel = gemm_kernel<K::bm, K::bn, K::wm, K::wn, ACOL, BCOL, EPI, T, ACT, PLA, PL, HP>;
   allow_lds(kernel, lds);
   check_grid(p.tiles_m * p.tiles_n * p.splits);
   kernel<<<dim3(unsigned(p.tiles_m * p.tiles_n * p.splits)), dim3(K::wm * K::wn * WAVE), lds,
@@ -309,30 +310,33 @@ void launch_config(GemmArgs& p, hipStream_t stream) {
   FD_LAUNCH_CHECK();
 }
 
-template <bool ACOL, bool BCOL, int EPI, class T, int ACT>
+template <bool ACOL, bool BCOL, int EPI, class T, int ACT, int HP>
 void launch(int config, GemmArgs& p, hipStream_t stream) {
-  if (config == BIG) launch_config<BIG, ACOL, BCOL, EPI, T, ACT>(p, stream);
-  else if (config == MID) launch_config<MID, ACOL, BCOL, EPI, T, ACT>(p, stream);
-  else launch_config<SMALL, ACOL, BCOL, EPI, T, ACT>(p, stream);
+  if constexpr (HP == planes_of<T>) {
+    if (config == BIG) return launch_config<BIG, ACOL, BCOL, EPI, T, ACT, HP>(p, stream);
+    if (config == MID) return launch_config<MID, ACOL, BCOL, EPI, T, ACT, HP>(p, stream);
+  }
+  launch_config<SMALL, ACOL, BCOL, EPI, T, ACT, HP>(p, stream);
 }
 
 // GATE or GRAD in the tile and parts of a plan, and the rest where there are parts.
-template <bool BCOL, int EPI, class T, int ACT>
+template <bool BCOL, int EPI, class T, int ACT, int HP>
 void launch_inner(int config, const Shape& s, float* part, GemmArgs& p, hipStream_t stream) {
   p.splits = s.splits;
   p.part = part;
-  launch<false, BCOL, EPI, T, ACT>(config, p, stream);
+  launch<false, BCOL, EPI, T, ACT, HP>(config, p, stream);
   if (s.splits == 1) return;
   const int64_t groups = ceil_div(ceil_div(p.M, 32) * (p.Fp / 32), GROUP / WAVE);
   check_grid(groups);
-  finish_kernel<EPI, T, ACT><<<dim3(unsigned(groups)), dim3(GROUP), 0, stream>>>(p);
+  finish_kernel<EPI, T, ACT, HP><<<dim3(unsigned(groups)), dim3(GROUP), 0, stream>>>(p);
   FD_LAUNCH_CHECK();
 }
 
-template <int C, class T>
+template <int C, class T, int HP>
 void launch_group(GemmGroup& s, hipStream_t stream) {
   using K = Config<C, STORE, T>;
-  constexpr size_t lds = gemm_lds<K::bm, K::bn, K::wm, K::wn, T>;
+  constexpr size_t lds = gemm_lds<K::bm, K::bn, T, HP, planes_of<T>>;
+  static_assert(K::bm == K::bn || HP == planes_of<T>, "the same LDS for planes of a and of b");
   int64_t at = 0;
   for (int i = 0; i < s.count; ++i) {
     GemmArgs& p = s.g[i];
@@ -343,7 +347,7 @@ void launch_group(GemmGroup& s, hipStream_t stream) {
   }
   s.first[s.count] = at;
   check_grid(at);
-  auto kernel = gemm_group_kernel<K::bm, K::bn, K::wm, K::wn, T>;
+  auto kernel = gemm_group_kernel<K::bm, K::bn, K::wm, K::wn, T, HP>;
   allow_lds(kernel, lds);
   kernel<<<dim3(unsigned(at)), dim3(K::wm * K::wn * WAVE), lds, stream>>>(s);
   FD_LAUNCH_CHECK();
@@ -420,6 +424,18 @@ void shapes_grad(const fd_gated_block& b, Shape (&s)[GROUP_GEMMS]) {
   s[2] = Shape{b.O, b.F, nt};
 }
 
+// Planes of H, dG and dU.  One bfloat16 plane rounds them once more than 32-bit
+// sums would, which adds as much error to Y and to the gradients as their own
+// last rounding (0.0024 from the float64 values and not 0.0017).  Where the products
+// are not what takes the time, what was rounded off is a second plane: 19 -> 19.4 us at
+// 2 x 32 -> 32 -> 28 (forward and backward), 29 -> 30 at 64 x 128 -> 256 -> 128,
+// 31 -> 33 at 256 x 128 -> 512 -> 128; but 42 -> 52 at 1,024 x 256 -> 512 -> 256, and 147
+// -> 232 at 5,003 x 509 -> 1365 -> 509, which keep one.
+constexpr double FINE_WORK = double(1 << 25);
+bool fine(const fd_gated_block& b) {
+  return b.type == FD_BF16 && double(b.N) * double(b.F) * double(std::max(b.D, b.O)) <= FINE_WORK;
+}
+
 template <class T>
 Work carve_work_t(Arena& a, const fd_gated_block& b, int backward) {
   Work w;
@@ -429,32 +445,34 @@ Work carve_work_t(Arena& a, const fd_gated_block& b, int backward) {
   w.wd = a.take<bf16>(packed<T>(b.O, b.F));
   const int64_t Fp = f_padded(b.F);
   const size_t blocks = size_t(ceil_div(b.N, 32)) * size_t(Fp / 32);
-  w.h = a.take<bf16>(size_t(b.N) * Fp * planes_of<T>);
+  const bool two = fine(b);
+  const int inner = two ? 2 : planes_of<T>;
+  w.h = a.take<bf16>(size_t(b.N) * Fp * inner);  // (few rows of float32: as they are)
   size_t part = 0;
   if (backward != 1) {
     w.gate = Shape{b.N, 2 * b.F, ceil_div(b.D, k_tile<T>)};
-    w.gate_config = plan<T>(&w.gate, 1, true, GATE, false);
+    w.gate_config = plan<T>(&w.gate, 1, two, GATE, false);
     if (w.gate.splits > 1) part = size_t(w.gate.splits) * blocks * 2048;
   }
   if (backward == 0) {
     w.shapes[0] = shape_y<T>(b);
-    w.config = plan<T>(w.shapes, 1, true, STORE, false);
+    w.config = plan<T>(w.shapes, 1, two, STORE, false);
     part = std::max(part, w.shapes[0].part());
     if (b.D <= NARROW && b.O <= NARROW)
       part = std::max(part, size_t(narrow_parts(b.N, b.F)) * size_t(b.N) * size_t(round_up(b.O, 4)));
   } else {
     w.dy = a.take<bf16>(packed<T>(b.N, b.O));
-    w.dgu = a.take<bf16>(size_t(b.N) * 2 * Fp * planes_of<T>);
+    w.dgu = a.take<bf16>(size_t(b.N) * 2 * Fp * inner);
     // a row for each 32 rows, or each row of waves of a tile: tiles of 64 or 128
     // rows have two, of 256 rows at most four
     w.colsum = a.take<float>(size_t(2 * ceil_div(b.N, 64) + 2) * 2 * Fp);
     w.dysum = a.take<float>(size_t(SUM_PARTS) * size_t(b.O));
     shapes_grad<T>(b, w.shapes);
-    w.config = plan<T>(w.shapes, GROUP_GEMMS, true, STORE, true);
+    w.config = plan<T>(w.shapes, GROUP_GEMMS, two, STORE, true);
     size_t sum = 0;
     for (const Shape& s : w.shapes) sum += s.part();
     w.grad = Shape{b.N, b.F, ceil_div(b.O, k_tile<T>)};
-    w.grad_config = plan<T>(&w.grad, 1, true, GRAD, true);
+    w.grad_config = plan<T>(&w.grad, 1, two, GRAD, true);
     part = std::max({part, sum, w.grad.splits > 1 ? size_t(w.grad.splits) * blocks * 1024 : 0});
     if (backward == 2) w.saved = a.take<char>(saved_bytes(b));
   }
@@ -503,7 +521,7 @@ Operand rows_of(const Matrix& m) { return Operand{{m.p, nullptr}, m.ld, m.plane,
 Operand columns_of(const Matrix& m) { return Operand{{m.p, nullptr}, m.ld, m.plane, m.cols, m.rows}; }
 
 // G, U (kept where `saved`) and H (where `h`).
-template <class T>
+template <class T, int HP>
 void run_gate(const fd_gated_block& b, const Work& w, const Matrix& x, const Matrix& wg,
               const Matrix& wu, char* saved, bool h, hipStream_t st) {
   GemmArgs p{};
@@ -520,8 +538,9 @@ void run_gate(const fd_gated_block& b, const Work& w, const Matrix& x, const Mat
   p.Fp = f_padded(b.F);
   p.H = h ? w.h : nullptr;
   p.hplane = b.N * p.Fp;
-  if (b.act == FD_ACT_SILU) launch_inner<false, GATE, T, FD_ACT_SILU>(w.gate_config, w.gate, w.part, p, st);
-  else launch_inner<false, GATE, T, FD_ACT_GELU>(w.gate_config, w.gate, w.part, p, st);
+  const auto run = b.act == FD_ACT_SILU ? launch_inner<false, GATE, T, FD_ACT_SILU, HP>
+                                        : launch_inner<false, GATE, T, FD_ACT_GELU, HP>;
+  run(w.gate_config, w.gate, w.part, p, st);
 }
 
 void check_block(const fd_gated_block* bp) {
@@ -580,21 +599,26 @@ void bring_weights(Work& w, const fd_gated_block& b, Matrix& wg, Matrix& wu) {
   }
 }
 
-template <class T>
+template <class T, int HP>
 void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void* Y, int64_t ldy,
              char* saved, hipStream_t st) {
   const int t = b.type;
   if (b.N <= skinny_rows<T> && saved == nullptr) {
-    SkinnyArgs p{b.X, b.Wg, b.Wu, b.ldx, b.ldwi, b.N, b.F, b.D, b.bg, b.bu, nullptr, 0, w.h, b.F};
-    if (b.act == FD_ACT_SILU) launch_skinny<T, true, FD_ACT_SILU>(p, st);
-    else launch_skinny<T, true, FD_ACT_GELU>(p, st);
-    p = SkinnyArgs{w.h, b.Wd, nullptr, b.F, b.ldwd, b.N, b.O, b.F, b.bd, nullptr, R, ldr, Y, ldy};
-    launch_skinny<T, false, 0>(p, st);
+    const int64_t Fp = f_padded(b.F), plane = b.N * Fp;
+    SkinnyArgs p{b.X,  b.Wg,    b.Wu, b.ldx, b.ldwi, b.N, b.F, b.D,
+                 b.bg, b.bu, nullptr,     0,    w.h,  Fp,   0, plane};
+    constexpr int SP = sizeof(T) == 4 ? 1 : HP;
+    if (b.act == FD_ACT_SILU) launch_skinny<T, SP, true, FD_ACT_SILU>(p, st);
+    else launch_skinny<T, SP, true, FD_ACT_GELU>(p, st);
+    p = SkinnyArgs{w.h,  b.Wd,    nullptr, Fp,  b.ldwd, b.N, b.O,   b.F,
+                   b.bd, nullptr, R,       ldr, Y,      ldy, plane, 0};
+    launch_skinny<T, SP, false, 0>(p, st);
     return;
   }
   if (b.D <= NARROW && b.O <= NARROW) {
-    NarrowArgs p{b, R, ldr, Y, ldy, saved, f_padded(b.F), narrow_parts(b.N, b.F), w.part, round_up(b.O, 4)};
-    run_narrow(p, st);
+    NarrowArgs p{b,      R,    ldr, Y, ldy, saved, f_padded(b.F), narrow_parts(b.N, b.F),
+                 w.part, round_up(b.O, 4)};
+    run_narrow(p, HP, st);
     if (p.parts == 1) return;
     AfterJobs after;
     after.splits = 1;
@@ -608,7 +632,7 @@ void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void*
   bring_weights(w, b, wg, wu);
   const Matrix wd = bring(w, b.Wd, b.ldwd, b.O, b.F, t, w.wd);
   run_before<T>(w.jobs, st);
-  run_gate<T>(b, w, x, wg, wu, saved, true, st);
+  run_gate<T, HP>(b, w, x, wg, wu, saved, true, st);
   const int64_t Fp = f_padded(b.F);
   GemmArgs p{};
   p.a = rows_of(Matrix{w.h, Fp, b.N, Fp, b.N * Fp});
@@ -626,7 +650,7 @@ void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void*
   AfterJobs after;
   float* room = w.part;
   set_parts(p, w.shapes[0], room, after);
-  launch<false, false, STORE, T, 0>(w.config, p, st);
+  launch<false, false, STORE, T, 0, HP>(w.config, p, st);
   run_after<T>(after, st);
 }
 
@@ -639,7 +663,7 @@ void clear(void* p, int64_t rows, int64_t cols, int64_t ld, hipStream_t st) {
   FD_LAUNCH_CHECK();
 }
 
-template <class T>
+template <class T, int HP>
 void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, char* saved,
               const fd_gated_grads& g, hipStream_t st) {
   const int t = b.type;
@@ -678,7 +702,7 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
   GemmGroup group{};
   if (inner) {
     if (gate) {
-      run_gate<T>(b, w, x, wg, wu, w.saved, false, st);
+      run_gate<T, HP>(b, w, x, wg, wu, w.saved, false, st);
       saved = w.saved;
     }
     GemmArgs p{};  // dH, and from it dG, dU, H
@@ -695,8 +719,9 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
     p.dGU = w.dgu;
     p.gplane = b.N * 2 * Fp;
     p.colsum = g.dbg != nullptr || g.dbu != nullptr ? w.colsum : nullptr;
-    if (b.act == FD_ACT_SILU) launch_inner<true, GRAD, T, FD_ACT_SILU>(w.grad_config, w.grad, w.part, p, st);
-    else launch_inner<true, GRAD, T, FD_ACT_GELU>(w.grad_config, w.grad, w.part, p, st);
+    const auto run = b.act == FD_ACT_SILU ? launch_inner<true, GRAD, T, FD_ACT_SILU, HP>
+                                          : launch_inner<true, GRAD, T, FD_ACT_GELU, HP>;
+    run(w.grad_config, w.grad, w.part, p, st);
     const int64_t sum_rows = w.grad.splits > 1
                                  ? ceil_div(b.N, 32)
                                  : p.tiles_m * grad_wave_rows<T>(w.grad_config);
@@ -740,7 +765,7 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
       q.out[0] = g.dWd;
       q.ldo = g.lddwd;
       q.half = q.rows = b.O;
-      group.acol[group.count] = true;
+      group.acol[group.count] = group.inner[group.count] = true;
       shapes[group.count++] = w.shapes[2];
     }
     if (group.count > 0) {
@@ -750,9 +775,12 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
         group.g[i].N = shapes[i].N;
         set_parts(group.g[i], shapes[i], room, after);
       }
-      if (w.config == BIG) launch_group<BIG, T>(group, st);
-      else if (w.config == MID) launch_group<MID, T>(group, st);
-      else launch_group<SMALL, T>(group, st);
+      auto run = launch_group<SMALL, T, HP>;
+      if constexpr (HP == planes_of<T>) {
+        if (w.config == BIG) run = launch_group<BIG, T, HP>;
+        if (w.config == MID) run = launch_group<MID, T, HP>;
+      }
+      run(group, st);
     }
     if (g.dbg != nullptr || g.dbu != nullptr)
       add_columns(after, w.colsum, sum_rows, 2 * Fp, Fp, b.F, g.dbg, g.dbu);
@@ -809,9 +837,11 @@ fd_status fd_gated_forward(const fd_gated_block* b, const void* R, int64_t ldr, 
     Work w = carve_checked(*b, 0, ws, ws_bytes);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (b->type == FD_F32)
-      forward<float>(*b, w, R, ldr, Y, ldy, static_cast<char*>(saved), st);
+      forward<float, 3>(*b, w, R, ldr, Y, ldy, static_cast<char*>(saved), st);
+    else if (fine(*b))
+      forward<bf16, 2>(*b, w, R, ldr, Y, ldy, static_cast<char*>(saved), st);
     else
-      forward<bf16>(*b, w, R, ldr, Y, ldy, static_cast<char*>(saved), st);
+      forward<bf16, 1>(*b, w, R, ldr, Y, ldy, static_cast<char*>(saved), st);
   });
 }
 
@@ -836,10 +866,13 @@ fd_status fd_gated_backward(const fd_gated_block* b, const void* dY, int64_t ldd
     Work w;
     if (b->N > 0) w = carve_checked(*b, saved == nullptr ? 2 : 1, ws, ws_bytes);
     hipStream_t st = static_cast<hipStream_t>(stream);
+    char* kept = static_cast<char*>(const_cast<void*>(saved));
     if (b->type == FD_F32)
-      backward<float>(*b, w, dY, lddy, static_cast<char*>(const_cast<void*>(saved)), g, st);
+      backward<float, 3>(*b, w, dY, lddy, kept, g, st);
+    else if (fine(*b))
+      backward<bf16, 2>(*b, w, dY, lddy, kept, g, st);
     else
-      backward<bf16>(*b, w, dY, lddy, static_cast<char*>(const_cast<void*>(saved)), g, st);
+      backward<bf16, 1>(*b, w, dY, lddy, kept, g, st);
   });
 }
 

@@ -52,7 +52,7 @@ __device__ __forceinline__ typename Eight<T>::Vec load_eight(const T* p, int64_t
 // 493.  Bound by the vector unit (activations, splitting into planes) about as
 // much as by the matrix unit.  The NW waves of a workgroup share the weights, widened
 // to planes on their way to LDS one step of F ahead; any alignment will do.
-template <class T, int DP, int OP, int NW, int ACT>
+template <class T, int DP, int OP, int NW, int ACT, int HP>
 __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
   constexpr int PL = planes_of<T>, KS = DP / 16, OB = OP / 32, THREADS = NW * WAVE;
   // LDS rows of DP (32) values, 16 bytes more apart: eight rows' same chunk cover all banks
@@ -118,28 +118,14 @@ __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = e < valid ? widen(T(raw[i][e])) : 0.f;
       if (q < 8 * DP)
-        write_planes<T>(&to.w[0][q / (4 * DP)][q % (4 * DP) / (DP / 8)][q % (DP / 8) * 8], 2 * 32 * WP, v);
+        write_planes<PL>(&to.w[0][q / (4 * DP)][q % (4 * DP) / (DP / 8)][q % (DP / 8) * 8], 2 * 32 * WP, v);
       else if (q < CHUNKS)
-        write_planes<T>(&to.d[0][(q - 8 * DP) / 4][(q - 8 * DP) % 4 * 8], OP * VP, v);
+        write_planes<PL>(&to.d[0][(q - 8 * DP) / 4][(q - 8 * DP) % 4 * 8], OP * VP, v);
     });
     if (threadIdx.x < 64) to.bias[threadIdx.x / 32][threadIdx.x % 32] = widen(bias);
   };
-  auto split = [](const float* x, bf16x8 (&out)[PL]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (PL == 3) {
-        bf16 u, v, w;
-        split3(x[i], u, v, w);
-        out[0][i] = u;
-        out[1][i] = v;
-        out[2][i] = w;
-      } else {
-        out[0][i] = bf16(x[i]);
-      }
-    }
-  };
-  constexpr int PAIRS = PL == 1 ? 1 : 6;
-  constexpr int PA[6] = {1, 0, 2, 0, 1, 0}, PB[6] = {1, 2, 0, 1, 0, 0};
+  using P = Pairs<PL, PL>;
+  using Q = Pairs<HP, PL>;
 
   fetch(f_first);
   bf16x8 x[KS][PL];
@@ -148,7 +134,7 @@ __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
     float v[8];
     const int k = s * 16 + half * 8;
     load_wide<8>(static_cast<const T*>(b.X) + min(m, b.N - 1) * b.ldx + k, int(b.D) - k, v);
-    split(v, x[s]);
+    to_planes<PL>(v, x[s]);
   }
   floatx16 y[OB];
 #pragma unroll
@@ -174,11 +160,11 @@ __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
         wu[q] = *reinterpret_cast<const bf16x8*>(&w.w[q][1][lane % 32][s * 16 + half * 8]);
       }
 #pragma unroll
-      for (int q = 0; q < PAIRS; ++q) {
-        floatx16 &tg = q + 1 == PAIRS ? g : gl, &tu = q + 1 == PAIRS ? u : ul;
-        const bf16x8 xs = x[s][PL == 1 ? 0 : PA[q]];
-        tg = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wg[PL == 1 ? 0 : PB[q]], xs, tg, 0, 0, 0);
-        tu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wu[PL == 1 ? 0 : PB[q]], xs, tu, 0, 0, 0);
+      for (int q = 0; q < P::COUNT; ++q) {
+        floatx16 &tg = q + 1 == P::COUNT ? g : gl, &tu = q + 1 == P::COUNT ? u : ul;
+        const bf16x8 xs = x[s][P::a(q)];
+        tg = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wg[P::b(q)], xs, tg, 0, 0, 0);
+        tu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wu[P::b(q)], xs, tu, 0, 0, 0);
       }
     }
     if (PL > 1) {
@@ -207,8 +193,8 @@ __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
     for (int e = 0; e < 16; ++e) h[e] = activate<ACT>(g[e]).value * u[e];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      bf16x8 hp[PL];
-      split(h + 8 * s, hp);
+      bf16x8 hp[HP];
+      to_planes<HP>(h + 8 * s, hp);
       bf16x8 wd[OB][PL];
 #pragma unroll
       for (int o = 0; o < OB; ++o)
@@ -219,11 +205,10 @@ __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
           wd[o][q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         }
 #pragma unroll
-      for (int q = 0; q < PAIRS; ++q)
+      for (int q = 0; q < Q::COUNT; ++q)
 #pragma unroll
         for (int o = 0; o < OB; ++o)
-          y[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              wd[o][PL == 1 ? 0 : PB[q]], hp[PL == 1 ? 0 : PA[q]], y[o], 0, 0, 0);
+          y[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wd[o][Q::b(q)], hp[Q::a(q)], y[o], 0, 0, 0);
     }
     // the other buffer was last read before this step's barrier
     if (f0 + 32 < f_last) put(buf[cur ^ 1], f0 + 32);
@@ -257,33 +242,34 @@ __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
     }
 }
 
-template <class T, int DP, int OP, int ACT>
+template <class T, int DP, int OP, int ACT, int HP>
 void launch(const NarrowArgs& p, hipStream_t stream) {
   constexpr int NW = NARROW_ROWS / 32;
   const dim3 grid(unsigned(ceil_div(p.b.N, NARROW_ROWS)), unsigned(p.parts));
-  narrow_kernel<T, DP, OP, NW, ACT><<<grid, dim3(NW * WAVE), 0, stream>>>(p);
+  narrow_kernel<T, DP, OP, NW, ACT, HP><<<grid, dim3(NW * WAVE), 0, stream>>>(p);
   FD_LAUNCH_CHECK();
 }
 
-template <class T, int ACT>
+template <class T, int ACT, int HP>
 void launch_narrow(const NarrowArgs& p, hipStream_t stream) {
-  if (p.b.D <= 32 && p.b.O <= 32) launch<T, 32, 32, ACT>(p, stream);
-  else if (p.b.D <= 32) launch<T, 32, 64, ACT>(p, stream);
-  else if (p.b.O <= 32) launch<T, 64, 32, ACT>(p, stream);
-  else launch<T, 64, 64, ACT>(p, stream);
+  if (p.b.D <= 32 && p.b.O <= 32) launch<T, 32, 32, ACT, HP>(p, stream);
+  else if (p.b.D <= 32) launch<T, 32, 64, ACT, HP>(p, stream);
+  else if (p.b.O <= 32) launch<T, 64, 32, ACT, HP>(p, stream);
+  else launch<T, 64, 64, ACT, HP>(p, stream);
 }
 
-template <class T>
+template <class T, int HP>
 void by_act(const NarrowArgs& p, hipStream_t stream) {
-  if (p.b.act == FD_ACT_SILU) launch_narrow<T, FD_ACT_SILU>(p, stream);
-  else launch_narrow<T, FD_ACT_GELU>(p, stream);
+  if (p.b.act == FD_ACT_SILU) launch_narrow<T, FD_ACT_SILU, HP>(p, stream);
+  else launch_narrow<T, FD_ACT_GELU, HP>(p, stream);
 }
 
 }  // namespace
 
-void run_narrow(const NarrowArgs& p, hipStream_t stream) {
-  if (p.b.type == FD_F32) by_act<float>(p, stream);
-  else by_act<bf16>(p, stream);
+void run_narrow(const NarrowArgs& p, int planes, hipStream_t stream) {
+  if (p.b.type == FD_F32) by_act<float, 3>(p, stream);
+  else if (planes == 2) by_act<bf16, 2>(p, stream);
+  else by_act<bf16, 1>(p, stream);
 }
 
 }  // namespace net

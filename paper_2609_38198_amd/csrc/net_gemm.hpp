@@ -235,7 +235,7 @@ struct GemmArgs {
   const void *bg, *bu;  // of the block's type, or NULL
   char* saved;          // G and U by 32 x 32 blocks, or NULL
   int64_t Fp;           // F rounded up to F_PAD: the planes' row length
-  bf16 *H, *dGU;        // N x Fp, N x 2 Fp
+  bf16 *H, *dGU;        // N x Fp, N x 2 Fp, HP planes each
   int64_t hplane, gplane;  // elements between planes
   float* colsum;        // 2 Fp column sums for each row of waves of each row tile, or NULL
 };
@@ -338,46 +338,70 @@ __device__ __forceinline__ void place(const GemmArgs& p, int64_t id, int64_t& tm
   tn = at / high;
 }
 
-template <class T>
-__device__ __forceinline__ void write_planes(bf16* p, int64_t plane, const float* x) {
-  bf16x8 a, b, c;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (sizeof(T) == 4) {
-      bf16 u, v, w;
-      split3(x[i], u, v, w);
-      a[i] = u;
-      b[i] = v;
-      c[i] = w;
-    } else {
-      a[i] = bf16(x[i]);
+// x as PL planes: rounded; rounded and the rest (16 bits or more); or all of it.
+template <int PL>
+__device__ __forceinline__ void to_planes(float x, bf16 (&out)[PL]) {
+  if constexpr (PL == 3) {
+    split3(x, out[0], out[1], out[2]);
+  } else {
+    out[0] = bf16(x);
+    if constexpr (PL == 2) {
+      const float rest = x - float(out[0]);
+      out[1] = bf16(fabsf(rest) < INFINITY ? rest : 0.f);  // an infinity stays one
     }
   }
-  *reinterpret_cast<bf16x8*>(p) = a;
-  if (sizeof(T) == 4) {
-    *reinterpret_cast<bf16x8*>(p + plane) = b;
-    *reinterpret_cast<bf16x8*>(p + 2 * plane) = c;
+}
+template <int PL>
+__device__ __forceinline__ void to_planes(const float* x, bf16x8 (&out)[PL]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    bf16 v[PL];
+    to_planes<PL>(x[i], v);
+#pragma unroll
+    for (int q = 0; q < PL; ++q) out[q][i] = v[q];
   }
 }
+template <int PL>
+__device__ __forceinline__ void write_planes(bf16* p, int64_t plane, const float* x) {
+  bf16x8 v[PL];
+  to_planes<PL>(x, v);
+#pragma unroll
+  for (int q = 0; q < PL; ++q) *reinterpret_cast<bf16x8*>(p + q * plane) = v[q];
+}
+
+// The plane pairs of a product that are worth their time, smallest first: all
+// with one plane on a side, of 3 x 3 those that reach 2^-24.
+template <int PLA, int PLB>
+struct Pairs {
+  static constexpr bool SIX = PLA == 3;
+  static_assert(SIX ? PLB == 3 : PLA * PLB <= 2, "1, 2 or 3 x 3 planes");
+  static constexpr int COUNT = SIX ? 6 : PLA * PLB;
+  static constexpr int six_a[6] = {1, 0, 2, 0, 1, 0}, six_b[6] = {1, 2, 0, 1, 0, 0};
+  static constexpr int a(int i) { return SIX ? six_a[i] : PLA == 2 ? 1 - i : 0; }
+  static constexpr int b(int i) { return SIX ? six_b[i] : PLB == 2 ? 1 - i : 0; }
+};
 
 // BM x BN tile of C by WM x WN waves of (BM / WM) x (BN / WN).  The matrix
 // instruction takes the n operand first, so that a lane holds four
 // consecutive n of one m: fragment value i is n = 8 (i / 4) + 4 (l / 32) + i % 4,
 // m = l % 32.
 //
-// id: the workgroup's number within the product.
-template <int BM, int BN, int WM, int WN, class T>
-constexpr size_t gemm_lds = 2 * (BM + BN) * k_tile<T> * 2 * planes_of<T>;
+// PLA, PLB: the operands' planes; HP: those of H, dG and dU.  id: the
+// workgroup's number within the product.
+template <int BM, int BN, class T, int PLA, int PLB>
+constexpr size_t gemm_lds = 2 * (BM * PLA + BN * PLB) * k_tile<T> * 2;
 
-template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, int EPI, class T, int ACT>
+template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, int EPI, class T, int ACT, int PLA,
+          int PLB, int HP>
 __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* smem) {
-  constexpr int THREADS = WM * WN * WAVE, KT = k_tile<T>, PL = planes_of<T>;
+  constexpr int THREADS = WM * WN * WAVE, KT = k_tile<T>;
+  using P = Pairs<PLA, PLB>;
   constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
   constexpr int BH = EPI == GATE ? BN / 2 : BN;  // extent of one b operand
-  using TA = Tile<BM, KT, PL, THREADS, ACOL>;
-  using TB = Tile<BH, KT, PL, THREADS, BCOL>;
+  using TA = Tile<BM, KT, PLA, THREADS, ACOL>;
+  using TB = Tile<BH, KT, PLB, THREADS, BCOL>;
   constexpr int BUF = TA::BYTES + TB::BYTES * (EPI == GATE ? 2 : 1);
-  static_assert(2 * BUF == gemm_lds<BM, BN, WM, WN, T>, "the launch's size");
+  static_assert(2 * BUF == gemm_lds<BM, BN, T, PLA, PLB>, "the launch's size");
   static_assert(EPI != GATE || FN % 2 == 0, "gate and up fragments in pairs");
 
   int64_t tm, tn;
@@ -430,7 +454,7 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
   const int wm = wave / WN, wn = wave % WN;
   // Three planes: the five smaller pairs have sums of their own, so that the
   // large one is rounded once a k step and not six times.
-  floatx16 acc[FM][FN], low[PL == 1 ? 1 : FM][PL == 1 ? 1 : FN];
+  floatx16 acc[FM][FN], low[P::SIX ? FM : 1][P::SIX ? FN : 1];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -438,47 +462,46 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         acc[i][j][e] = 0.f;
-        if (PL > 1) low[i][j][e] = 0.f;
+        if (P::SIX) low[i][j][e] = 0.f;
       }
 
   // Fragments of k step ks of the tile in a buffer.  GATE: the first half of the n
   // fragments are gate columns, the others the same up columns.
-  bf16x8 fa[2][PL][FM], fb[2][PL][FN];
+  bf16x8 fa[2][PLA][FM], fb[2][PLB][FN];
   auto read = [&](int into, int buf, int ks) {
     const char* sa = smem + buf * BUF;
     const char* sb = sa + TA::BYTES;
 #pragma unroll
-    for (int q = 0; q < PL; ++q) {
+    for (int q = 0; q < (PLA > PLB ? PLA : PLB); ++q) {
 #pragma unroll
       for (int i = 0; i < FM; ++i)
-        fa[into][q][i] = TA::fragment(sa + q * TA::PLANE, wm * TM + i * 32, ks);
+        if (q < PLA) fa[into][q][i] = TA::fragment(sa + q * TA::PLANE, wm * TM + i * 32, ks);
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
+        if (q >= PLB) continue;
         constexpr int HALF = EPI == GATE ? FN / 2 : FN;
         fb[into][q][j] = TB::fragment(sb + (j / HALF) * TB::BYTES + q * TB::PLANE,
                                       wn * HALF * 32 + (j % HALF) * 32, ks);
       }
     }
   };
-  // The plane pairs of x y that reach 2^-24 of it, smallest first.
   auto multiply = [&](int from) {
-    constexpr int PAIRS = PL == 1 ? 1 : 6;
-    constexpr int PA[6] = {1, 0, 2, 0, 1, 0}, PB[6] = {1, 2, 0, 1, 0, 0};
 #pragma unroll
-    for (int q = 0; q < PAIRS; ++q)
+    for (int q = 0; q < P::COUNT; ++q)
 #pragma unroll
       for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-          floatx16& to = q + 1 == PAIRS ? acc[i][j] : low[PL == 1 ? 0 : i][PL == 1 ? 0 : j];
-          to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              fb[from][PL == 1 ? 0 : PB[q]][j], fa[from][PL == 1 ? 0 : PA[q]][i], to, 0, 0, 0);
+          floatx16& to =
+              P::SIX && q + 1 < P::COUNT ? low[P::SIX ? i : 0][P::SIX ? j : 0] : acc[i][j];
+          to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[from][P::b(q)][j], fa[from][P::a(q)][i],
+                                                       to, 0, 0, 0);
         }
   };
   // The scheduler's order within a step: LDS reads evenly among the products.
   auto interleave = [] {
-    constexpr int READS = PL * (FM * (ACOL ? 2 : 1) + FN * (BCOL ? 2 : 1));
-    constexpr int MULS = FM * FN * (PL == 1 ? 1 : 6);
+    constexpr int READS = PLA * FM * (ACOL ? 2 : 1) + PLB * FN * (BCOL ? 2 : 1);
+    constexpr int MULS = FM * FN * P::COUNT;
 #pragma unroll
     for (int i = 0; i < MULS; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x100, (READS + MULS - 1) / MULS, 0);
@@ -518,11 +541,11 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
       interleave();
     }
   }
-  if (PL > 1) {
+  if (P::SIX) {
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] += low[PL == 1 ? 0 : i][PL == 1 ? 0 : j];
+      for (int j = 0; j < FN; ++j) acc[i][j] += low[P::SIX ? i : 0][P::SIX ? j : 0];
   }
   __syncthreads();  // the buffers become the waves' staging slabs
 
@@ -612,7 +635,7 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
       if (mb + r >= p.M || nl >= p.Fp) continue;
       float x[8];
       get(r, x);
-      write_planes<T>(to + (mb + r) * ld + nl, plane, x);
+      write_planes<HP>(to + (mb + r) * ld + nl, plane, x);
     }
   };
 
@@ -748,10 +771,11 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
   }
 }
 
-template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, int EPI, class T, int ACT>
+template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, int EPI, class T, int ACT, int PLA,
+          int PLB, int HP>
 __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
   extern __shared__ __align__(1024) char smem[];
-  gemm_body<BM, BN, WM, WN, ACOL, BCOL, EPI, T, ACT>(p, blockIdx.x, smem);
+  gemm_body<BM, BN, WM, WN, ACOL, BCOL, EPI, T, ACT, PLA, PLB, HP>(p, blockIdx.x, smem);
 }
 
 // The backward pass's last products, which do not depend on each other, in one
@@ -760,25 +784,29 @@ constexpr int GROUP_GEMMS = 3;
 struct GemmGroup {
   GemmArgs g[GROUP_GEMMS];
   bool acol[GROUP_GEMMS];          // a in column order (b always is)
+  bool inner[GROUP_GEMMS];         // b, and not a, has HP planes
   int64_t first[GROUP_GEMMS + 1];  // a product's first workgroup
   int count;
 };
 
-template <int BM, int BN, int WM, int WN, class T>
+template <int BM, int BN, int WM, int WN, class T, int HP>
 __global__ __launch_bounds__(WM * WN * WAVE) void gemm_group_kernel(GemmGroup s) {
   extern __shared__ __align__(1024) char smem[];
   int i = 0;
   while (i + 1 < s.count && s.first[i + 1] <= int64_t(blockIdx.x)) ++i;
   const int64_t id = int64_t(blockIdx.x) - s.first[i];
-  if (s.acol[i])
-    gemm_body<BM, BN, WM, WN, true, true, STORE, T, 0>(s.g[i], id, smem);
-  else
-    gemm_body<BM, BN, WM, WN, false, true, STORE, T, 0>(s.g[i], id, smem);
+  constexpr int PL = planes_of<T>;
+  if (!s.acol[i])
+    gemm_body<BM, BN, WM, WN, false, true, STORE, T, 0, HP, PL, HP>(s.g[i], id, smem);
+  else if (HP == PL || !s.inner[i])
+    gemm_body<BM, BN, WM, WN, true, true, STORE, T, 0, HP, PL, HP>(s.g[i], id, smem);
+  else if constexpr (HP != PL)
+    gemm_body<BM, BN, WM, WN, true, true, STORE, T, 0, PL, HP, HP>(s.g[i], id, smem);
 }
 
 // The rest of a GATE or GRAD product whose k is split: a wave to a 32 x 32 block
 // adds the parts in their order and goes on as the product's own epilogue does.
-template <int EPI, class T, int ACT>
+template <int EPI, class T, int ACT, int HP>
 __global__ __launch_bounds__(256) void finish_kernel(GemmArgs p) {
   constexpr int MATS = EPI == GATE ? 2 : 1;
   const int lane = threadIdx.x % WAVE, half32 = lane / 32;
@@ -848,22 +876,16 @@ __global__ __launch_bounds__(256) void finish_kernel(GemmArgs p) {
     const int64_t plane = w == 2 ? p.hplane : p.gplane;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      bf16x4 v[3];
+      bf16x4 v[HP];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float y = out[w][4 * q + e];
-        if (sizeof(T) == 4) {
-          bf16 a, b, c;
-          split3(y, a, b, c);
-          v[0][e] = a;
-          v[1][e] = b;
-          v[2][e] = c;
-        } else {
-          v[0][e] = bf16(y);
-        }
+        bf16 y[HP];
+        to_planes<HP>(out[w][4 * q + e], y);
+#pragma unroll
+        for (int k = 0; k < HP; ++k) v[k][e] = y[k];
       }
 #pragma unroll
-      for (int k = 0; k < planes_of<T>; ++k)
+      for (int k = 0; k < HP; ++k)
         *reinterpret_cast<bf16x4*>(to + k * plane + fb + 8 * q + 4 * half32) = v[k];
     }
   }

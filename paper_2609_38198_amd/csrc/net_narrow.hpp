@@ -32,7 +32,8 @@ struct NarrowArgs {
   int64_t ldp;
 };
 
-void run_narrow(const NarrowArgs& p, hipStream_t stream);
+// planes: of H, between its two products.
+void run_narrow(const NarrowArgs& p, int planes, hipStream_t stream);
 
 }  // namespace net
 }  // namespace fd

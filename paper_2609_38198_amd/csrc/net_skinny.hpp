@@ -24,6 +24,7 @@ struct SkinnyArgs {
   int64_t ldr;
   void* out;
   int64_t ldo;
+  int64_t xplane, plane;    // elements between planes of x, out
 };
 
 // A workgroup makes 16 columns of C for NB x 16 rows; its W waves share the
@@ -32,7 +33,9 @@ struct SkinnyArgs {
 // matrix in flight at once, every weight read once and by one wave.  The sum over the waves, in their
 // order, is in LDS.  1 x 1024 -> 4096 -> 1024 in bfloat16 moves 17 MB in 5.5 us and 8 MB in 7.0 us:
 // latency, of one trip to memory for each of the 64 workgroups' waves, more than bandwidth.
-template <class T, int NB, int W, bool GATED, int ACT>
+//
+// HP: the planes of H in bfloat16, which the first product writes and the second reads.
+template <class T, int HP, int NB, int W, bool GATED, int ACT>
 __global__ __launch_bounds__(W * WAVE) void skinny_kernel(SkinnyArgs p) {
   constexpr int MATS = GATED ? 2 : 1;
   constexpr int V = VEC<T>, KC = 8 * V;  // k of a step: two loads of 16 bytes by four lane groups
@@ -43,6 +46,7 @@ __global__ __launch_bounds__(W * WAVE) void skinny_kernel(SkinnyArgs p) {
   const T* w[MATS];
   w[0] = static_cast<const T*>(p.w) + f * p.ldw;
   if (GATED) w[MATS - 1] = static_cast<const T*>(p.up) + f * p.ldw;
+  constexpr int XP = GATED ? 1 : HP;
   const T* x[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i)
@@ -68,7 +72,7 @@ __global__ __launch_bounds__(W * WAVE) void skinny_kernel(SkinnyArgs p) {
   };
   auto step = [&](int64_t k0, bool whole) {
     // lane group l / 16 has k = k0 + 2 V (l / 16) + V j + 0 .. V - 1
-    Chunk cw[MATS][2], cx[NB][2];
+    Chunk cw[MATS][2], cx[NB][2][XP];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int64_t k = k0 + (lane / 16) * 2 * V + j * V;
@@ -76,7 +80,9 @@ __global__ __launch_bounds__(W * WAVE) void skinny_kernel(SkinnyArgs p) {
 #pragma unroll
       for (int m = 0; m < MATS; ++m) cw[m][j] = load(w[m] + k, left);
 #pragma unroll
-      for (int i = 0; i < NB; ++i) cx[i][j] = load(x[i] + k, left);
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int q = 0; q < XP; ++q) cx[i][j][q] = load(x[i] + q * p.xplane + k, left);
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -85,13 +91,15 @@ __global__ __launch_bounds__(W * WAVE) void skinny_kernel(SkinnyArgs p) {
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
           if constexpr (sizeof(T) == 2) {
-            acc[m][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                __builtin_bit_cast(bf16x8, cw[m][j]), __builtin_bit_cast(bf16x8, cx[i][j]),
-                acc[m][i], 0, 0, 0);
+#pragma unroll
+            for (int q = XP - 1; q >= 0; --q)
+              acc[m][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  __builtin_bit_cast(bf16x8, cw[m][j]), __builtin_bit_cast(bf16x8, cx[i][j][q]),
+                  acc[m][i], 0, 0, 0);
           } else {
 #pragma unroll
             for (int e = 0; e < V; ++e)
-              acc[m][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(cw[m][j].v[e], cx[i][j].v[e],
+              acc[m][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(cw[m][j].v[e], cx[i][j][0].v[e],
                                                                acc[m][i], 0, 0, 0);
           }
         }
@@ -121,32 +129,40 @@ __global__ __launch_bounds__(W * WAVE) void skinny_kernel(SkinnyArgs p) {
       s[0] = activate<ACT>(s[0]).value * s[MATS - 1];
     }
     if (p.R != nullptr) s[0] += widen(static_cast<const T*>(p.R)[row * p.ldr + col]);
-    static_cast<T*>(p.out)[row * p.ldo + col] = narrow<T>(s[0]);
+    T* out = static_cast<T*>(p.out) + row * p.ldo + col;
+    if constexpr (GATED && HP == 2) {
+      bf16 v[2];
+      to_planes<2>(s[0], v);
+      out[0] = v[0];
+      out[p.plane] = v[1];
+    } else {
+      *out = narrow<T>(s[0]);
+    }
   }
 }
 
 // As many waves as have a stretch of k each (a power of two).
-template <class T, int NB, bool GATED, int ACT>
+template <class T, int HP, int NB, bool GATED, int ACT>
 void launch_skinny_blocks(const SkinnyArgs& p, hipStream_t stream) {
   const int64_t stretches = ceil_div(p.K, 8 * VEC<T>);
   const dim3 grid(unsigned(ceil_div(p.F, int64_t(16))));
   if (SKINNY_WAVES / NB >= 16 && stretches > 8) {
     constexpr int W = SKINNY_WAVES / NB < 16 ? 1 : 16;
-    skinny_kernel<T, NB, W, GATED, ACT><<<grid, dim3(W * WAVE), 0, stream>>>(p);
+    skinny_kernel<T, HP, NB, W, GATED, ACT><<<grid, dim3(W * WAVE), 0, stream>>>(p);
   } else if (SKINNY_WAVES / NB >= 8 && stretches > 4) {
     constexpr int W = SKINNY_WAVES / NB < 8 ? 1 : 8;
-    skinny_kernel<T, NB, W, GATED, ACT><<<grid, dim3(W * WAVE), 0, stream>>>(p);
+    skinny_kernel<T, HP, NB, W, GATED, ACT><<<grid, dim3(W * WAVE), 0, stream>>>(p);
   } else {
-    skinny_kernel<T, NB, 4, GATED, ACT><<<grid, dim3(4 * WAVE), 0, stream>>>(p);
+    skinny_kernel<T, HP, NB, 4, GATED, ACT><<<grid, dim3(4 * WAVE), 0, stream>>>(p);
   }
   FD_LAUNCH_CHECK();
 }
 
-template <class T, bool GATED, int ACT>
+template <class T, int HP, bool GATED, int ACT>
 void launch_skinny(const SkinnyArgs& p, hipStream_t stream) {
-  if (p.n <= 16) launch_skinny_blocks<T, 1, GATED, ACT>(p, stream);
-  else if (p.n <= 32) launch_skinny_blocks<T, 2, GATED, ACT>(p, stream);
-  else launch_skinny_blocks<T, 4, GATED, ACT>(p, stream);
+  if (p.n <= 16) launch_skinny_blocks<T, HP, 1, GATED, ACT>(p, stream);
+  else if (p.n <= 32) launch_skinny_blocks<T, HP, 2, GATED, ACT>(p, stream);
+  else launch_skinny_blocks<T, HP, 4, GATED, ACT>(p, stream);
 }
 
 }  // namespace net
