@@ -31,7 +31,7 @@ struct SkinnyArgs {
 // columns and take every W-th stretch of k, whose weights go straight from
 // memory to the matrix operand: 16 rows x 64 k (float32: 32) of each
 // matrix in flight at once, every weight read once and by one wave.  The sum over the waves, in their
-// order, is in LDS.  1 x 1024 -> 4096 -> 1024 in bfloat16 moves 17 MB in 5.5 us and 8 MB in 7.0 us:
+// order, is in LDS.  1 x 1024 -> 4096 -> 1024 in bfloat16 moves 17 MB in 5.4 us and 8 MB in 7.8 us:
 // latency, of one trip to memory for each of the 64 workgroups' waves, more than bandwidth.
 //
 // HP: the planes of H in bfloat16, which the first product writes and the second reads.
