@@ -433,8 +433,7 @@ typedef struct fd_gated_grads {
 } fd_gated_grads;
 
 /* Bytes of the buffer that carries a forward pass's G and U (in the kernels' own
- * order; float32, or for bfloat16 11-bit values with a scale for each 32 x 32
- * of them) to the backward pass. */
+ * order; float32, for bfloat16 cut to its upper 24 bits) to the backward pass. */
 size_t fd_gated_saved_size(const fd_gated_block* b);
 
 /* Bytes of workspace of fd_gated_forward (backward = 0) or fd_gated_backward

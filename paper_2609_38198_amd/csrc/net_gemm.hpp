@@ -242,79 +242,70 @@ struct GemmArgs {
 
 // G and U are kept for the backward pass by 32 x 32 blocks in the accumulators'
 // own order, so that both sides move whole lines without a detour.  A float32
-// block keeps 4-byte values; a bfloat16 block 2-byte ones of 11 bits, scaled
-// by a power of two per block: 2^-12 of a value is lost, an eighth of what
-// the gradients' own rounding loses, for half of the bytes of the backward pass's
-// largest operand.
+// block keeps 4-byte values; a bfloat16 block the upper three bytes of each: all
+// of float32's range whatever lies beside a value, and less than 2^-15 of it cut
+// off, 1/64 of what the gradients' own rounding loses, for 3/4 of the bytes of the
+// backward pass's largest operand.
 template <class T>
-constexpr int64_t saved_block_bytes = sizeof(T) == 4 ? 8192 : 4096 + 16;
+constexpr int64_t saved_block_bytes = sizeof(T) == 4 ? 8192 : 6144;
 
 template <class T>
 __device__ __forceinline__ char* saved_at(char* saved, int64_t m, int64_t f, int64_t Fp) {
   return saved + ((m / 32) * (Fp / 32) + f / 32) * saved_block_bytes<T>;
 }
 
-typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+// One of a block's two arrays (which = 0: G, 1: U) lies in quads of 16 bytes a
+// lane, quad q of lane l at 16 (64 q + l).  float32: four values each.  bfloat16:
+// the upper halves of the values 0 to 7 and 8 to 15, then the third byte of each.
+template <class T>
+constexpr int kept_quads = sizeof(T) == 4 ? 4 : 3;
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 
-// One of a block's two arrays (which = 0: G, 1: U): lane l's values of a
-// quarter (float32) or half (bfloat16) of the block are 16 bytes at 16 l.
 template <class T>
 __device__ __forceinline__ void save16(char* block, int which, int lane, const floatx16& x) {
-  if (sizeof(T) == 4) {
+  uintx4 v[kept_quads<T>];
+  const auto bits = [&](int i) { return __builtin_bit_cast(uint32_t, float(x[i])); };
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const floatx4 v = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
-      *reinterpret_cast<floatx4*>(block + which * 4096 + (q * WAVE + lane) * 16) = v;
+  for (int i = 0; i < 16; i += 4) {
+    if constexpr (sizeof(T) == 4) {
+      v[i / 4] = uintx4{bits(i), bits(i + 1), bits(i + 2), bits(i + 3)};
+    } else {
+      // (a byte permutation takes bytes 0 to 3 of its second word as 0 to 3, of its first as 4 to 7)
+      v[i / 8][i % 8 / 2] = __builtin_amdgcn_perm(bits(i + 1), bits(i), 0x07060302);
+      v[i / 8][i % 8 / 2 + 1] = __builtin_amdgcn_perm(bits(i + 3), bits(i + 2), 0x07060302);
+      v[kept_quads<T> - 1][i / 4] = __builtin_amdgcn_perm(bits(i + 1), bits(i), 0x0c0c0501) |
+                                    __builtin_amdgcn_perm(bits(i + 3), bits(i + 2), 0x05010c0c);
     }
-    return;
   }
-  float top = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.f);
-  top = wave_max(top);
-  // 2^14 below the type's largest power, for blocks down to 2^-100
-  const int e = max(int(__builtin_bit_cast(uint32_t, top) >> 23), 27);
-  const float scale = __builtin_bit_cast(float, uint32_t(127 + 14 + 127 - e) << 23);
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    halfx8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = _Float16(x[8 * q + i] * scale);
-    *reinterpret_cast<halfx8*>(block + 16 + which * 2048 + (q * WAVE + lane) * 16) = v;
-  }
-  if (lane == 0)
-    *reinterpret_cast<float*>(block + which * 4) =
-        __builtin_bit_cast(float, uint32_t(e - 14) << 23);
+  for (int q = 0; q < kept_quads<T>; ++q)
+    *reinterpret_cast<uintx4*>(block + ((which * kept_quads<T> + q) * WAVE + lane) * 16) = v[q];
 }
 // The same, back: as it lies in memory (nothing waits for it yet), then widened.
 template <class T>
 struct Kept {
-  floatx4 v[sizeof(T) == 4 ? 4 : 2];
-  float scale;
+  uintx4 v[kept_quads<T>];
 };
 template <class T>
 __device__ __forceinline__ Kept<T> load_kept(const char* block, int which, int lane) {
   Kept<T> k;
-  constexpr int N = sizeof(T) == 4 ? 4 : 2;
-  const char* p = block + (sizeof(T) == 4 ? which * 4096 : 16 + which * 2048);
 #pragma unroll
-  for (int q = 0; q < N; ++q) k.v[q] = *reinterpret_cast<const floatx4*>(p + (q * WAVE + lane) * 16);
-  k.scale = sizeof(T) == 4 ? 1.f : *reinterpret_cast<const float*>(block + which * 4);
+  for (int q = 0; q < kept_quads<T>; ++q)
+    k.v[q] = *reinterpret_cast<const uintx4*>(block + ((which * kept_quads<T> + q) * WAVE + lane) * 16);
   return k;
 }
 template <class T>
 __device__ __forceinline__ floatx16 widen_kept(const Kept<T>& k) {
   floatx16 x;
-  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = k.v[i / 4][i % 4];
-  } else {
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const halfx8 v = __builtin_bit_cast(halfx8, k.v[q]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[8 * q + i] = float(v[i]) * k.scale;
-    }
+  for (int i = 0; i < 16; ++i) {
+    uint32_t w;
+    if constexpr (sizeof(T) == 4)
+      w = k.v[i / 4][i % 4];
+    else  // 0, the third byte, the upper half
+      w = __builtin_amdgcn_perm(k.v[i / 8][i % 8 / 2], k.v[kept_quads<T> - 1][i / 4],
+                                (i % 2 == 0 ? 0x0504000cu : 0x0706000cu) | uint32_t(i % 4) << 8);
+    x[i] = __builtin_bit_cast(float, w);
   }
   return x;
 }
