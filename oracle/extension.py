@@ -7,8 +7,9 @@ import numpy as np
 BLOCK = 256  # elements that share a scale of 8-bit states
 
 
-def _erf(x):
-    return np.vectorize(math.erf, otypes=[np.float64])(x)
+def _phi(x):
+    """The normal distribution function; by erfc, which keeps the lower tail."""
+    return 0.5 * np.vectorize(math.erfc, otypes=[np.float64])(-np.asarray(x) / math.sqrt(2.0))
 
 
 def layer_norm(X, gamma=None, beta=None, eps=1e-5):
@@ -41,7 +42,7 @@ def activation(g, act):
     if act == "silu":
         z = 1.0 / (1.0 + np.exp(-g))
         return g * z, z + g * z * (1.0 - z)
-    z = 0.5 * (1.0 + _erf(g / math.sqrt(2.0)))
+    z = _phi(g)
     return g * z, z + g * np.exp(-g * g / 2.0) / math.sqrt(2.0 * math.pi)
 
 

@@ -190,7 +190,7 @@ __global__ __launch_bounds__(NW * WAVE, 2) void narrow_kernel(NarrowArgs p) {
     // past F the weights and biases are zero, and so is H
     float h[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) h[e] = activate<ACT>(g[e]).value * u[e];
+    for (int e = 0; e < 16; ++e) h[e] = activate<ACT, T>(g[e]).value * u[e];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       bf16x8 hp[HP];

@@ -180,26 +180,52 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// act(g) and its derivative.
+// act(g) and its derivative, of pre-activations of a block of type T.
+//
+// SiLU's error is the exponential's argument's: |g| 2^-24 of the value far out.
+//
+// GELU: with x = |g| / sqrt 2, erfc(x) = exp(-x^2) t P(t), t = 1 / (1 + p x), which keeps
+// its relative accuracy in the tail, where Phi(g) is that difference from one and
+// nothing else.  The exponential is also the derivative's.  P and p are least-maximum fits of the
+// relative error for x up to 10.2, beyond which erfc has left float32: degree 8, 4.4e-8, for float32
+// (with x^2 in two words, or its rounding would be up to 1e-5 of the value: Phi to 4e-7
+// from -13 on); degree 4, 4e-5, for bfloat16, whose rounding is 2^-9.
 struct Act {
   float value, slope;
 };
-template <int ACT>
+template <int ACT, class T>
 __device__ __forceinline__ Act activate(float g) {
+  constexpr bool FULL = sizeof(T) == 4;
   Act a;
   if (ACT == FD_ACT_SILU) {
     const float z = __builtin_amdgcn_rcpf(1.f + __expf(-g));
     a.value = g * z;
     a.slope = z * (1.f + g * (1.f - z));
   } else {
-    // erfc by Hastings' rational fit (Abramowitz and Stegun 7.1.26, absolute
-    // error 1.5e-7), whose exponential is also the derivative's
-    const float x = fabsf(g) * 0.70710678f;
-    const float e = __expf(-x * x);
-    const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
-    const float c = e * t *
-                    (0.254829592f +
-                     t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    float e, t, q;
+    if (FULL) {
+      const float x = fminf(fabsf(g), 20.f);  // exp(-200) is zero, and nothing overflows
+      constexpr float K = 0.7213475f, K1 = 9.629815e-09f;  // log2(e) / 2 in two words
+      const float hi = x * x, lo = fmaf(x, x, -hi), u = hi * K;
+      const float rest = fmaf(hi, K1, fmaf(lo, K, fmaf(hi, K, -u)));
+      e = __builtin_amdgcn_exp2f(-u);
+      e = fmaf(-e, rest * 0.69314718f, e);
+      t = __builtin_amdgcn_rcpf(fmaf(x, 0.33587572f, 1.f));
+      constexpr float P[9] = {-0.04775394f, 0.26531526f, -0.5411254f, 0.42149332f, -0.09736633f,
+                              0.2351757f, 0.22727302f, 0.2690432f, 0.26794523f};
+      q = P[0];
+#pragma unroll
+      for (int i = 1; i < 9; ++i) q = fmaf(q, t, P[i]);
+    } else {
+      const float x = fabsf(g) * 0.70710678f;
+      e = __expf(-x * x);
+      t = __builtin_amdgcn_rcpf(fmaf(x, 0.525f, 1.f));
+      constexpr float P[5] = {-0.17918006f, 0.4112108f, 0.15910082f, 0.31389964f, 0.29500666f};
+      q = P[0];
+#pragma unroll
+      for (int i = 1; i < 5; ++i) q = fmaf(q, t, P[i]);
+    }
+    const float c = e * t * q;
     const float z = g < 0.f ? 0.5f * c : 1.f - 0.5f * c;
     a.value = g * z;
     a.slope = z + g * e * 0.39894228f;
@@ -693,7 +719,7 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const bool there = fb + 8 * (e / 4) + 4 * half32 + e % 4 < p.N;
-          h[e] = there ? activate<ACT>(g[e]).value * u[e] : 0.f;
+          h[e] = there ? activate<ACT, T>(g[e]).value * u[e] : 0.f;
         }
         put(j, h);
       }
@@ -723,7 +749,7 @@ __device__ __forceinline__ void gemm_body(const GemmArgs& p, int64_t id, char* s
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const bool there = live && fb + 8 * (e / 4) + 4 * half32 + e % 4 < p.N;
-            const Act a = activate<ACT>(g[e]);
+            const Act a = activate<ACT, T>(g[e]);
             const float dh = acc[i][j][e];
             v[0][j][e] = there ? dh * u[e] * a.slope : 0.f;
             v[1][j][e] = there ? dh * a.value : 0.f;
@@ -829,7 +855,7 @@ __global__ __launch_bounds__(256) void finish_kernel(GemmArgs p) {
         const int i = 4 * q + e;
         x[0][i] += bg[e];
         x[1][i] += bu[e];
-        out[2][i] = e < valid ? activate<ACT>(x[0][i]).value * x[1][i] : 0.f;
+        out[2][i] = e < valid ? activate<ACT, T>(x[0][i]).value * x[1][i] : 0.f;
       }
     }
     if (p.saved != nullptr) {
@@ -845,7 +871,7 @@ __global__ __launch_bounds__(256) void finish_kernel(GemmArgs p) {
     for (int e = 0; e < 16; ++e) {
       const int64_t f = fb + 8 * (e / 4) + 4 * half32 + e % 4;
       const bool there = m < p.M && f < p.N;
-      const Act a = activate<ACT>(g[e]);
+      const Act a = activate<ACT, T>(g[e]);
       const float dh = x[0][e];
       out[0][e] = there ? dh * u[e] * a.slope : 0.f;
       out[1][e] = there ? dh * a.value : 0.f;

@@ -126,7 +126,7 @@ __global__ __launch_bounds__(W * WAVE) void skinny_kernel(SkinnyArgs p) {
     if (p.b != nullptr) s[0] += widen(static_cast<const T*>(p.b)[col]);
     if (GATED) {
       if (p.bu != nullptr) s[MATS - 1] += widen(static_cast<const T*>(p.bu)[col]);
-      s[0] = activate<ACT>(s[0]).value * s[MATS - 1];
+      s[0] = activate<ACT, T>(s[0]).value * s[MATS - 1];
     }
     if (p.R != nullptr) s[0] += widen(static_cast<const T*>(p.R)[row * p.ldr + col]);
     T* out = static_cast<T*>(p.out) + row * p.ldo + col;

@@ -69,3 +69,52 @@ def test_a_large_row_leaves_its_own_small_features(dtype):
         at = np.s_[..., [3, 40]] if name == "dWd" else np.s_[[3, 40]]
         off = worst_lines(to_np(getattr(g, name))[at], want[name][0][at], want[name][1][at])
         assert max(off["row"], off["column"]) <= GATED_TOL[dtype], (name, off)
+
+
+# Phi's tail: the activation alone, act(g) = act(X[n, 0]) in every row, by each way through the
+# block: few rows, the narrow kernel, the tiles.  float32: some eight roundings of 2^-24 (the
+# polynomial's last steps, the exponential, the reciprocal, products), 16 x 2^-24 =
+# 9.5e-7 with room; SiLU's exponential has |g| 2^-24 more.  bfloat16: the inner and the last rounding.
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("n, d", [(30, 1), (4000, 1), (4000, 65)])
+def test_activation_in_its_tails(n, d, act, dtype):
+    dev = device()
+    X = torch.zeros(n, d, dtype=dtype, device=dev)
+    X[:, 0] = torch.linspace(-12.0, 8.0, n, device=dev).to(dtype)
+    Wg, Wu = torch.zeros(1, d, dtype=dtype, device=dev), torch.zeros(1, d, dtype=dtype, device=dev)
+    Wg[0, 0] = 1.0
+    one = torch.ones(1, 1, dtype=dtype, device=dev)
+    case(f"{act} of {n} values, {d} features, {dtype}")
+    Y, saved = fd.fd_gated_forward(X, Wg, Wu, one, bu=one[0], act=act, save=n > 30)
+    g = to_np(X)[:, 0]
+    # the negative branch by erfc, which the oracle's 1 + erf has lost at -6
+    import math
+    phi = np.array([0.5 * math.erfc(-x / math.sqrt(2.0)) for x in g])
+    z = phi if act == "gelu" else 1.0 / (1.0 + np.exp(-g))
+    tol = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24 * (16.0 + (np.abs(g) if act == "silu" else 0.0))
+    off = np.abs(to_np(Y)[:, 0] - g * z)
+    assert (off <= tol * np.abs(g * z)).all(), np.max(off / np.maximum(np.abs(g * z), 1e-300))
+    # dX = act'(g) where U does not depend on X; measured against its two terms
+    b = fd.fd_gated_backward(torch.ones_like(Y), X, Wg, Wu, one, bu=one[0], act=act, saved=saved)
+    rest = g * np.exp(-g * g / 2) / math.sqrt(2 * math.pi) if act == "gelu" else g * z * (1 - z)
+    off = np.abs(to_np(b.dX)[:, 0] - (z + rest))
+    assert (off <= tol * (np.abs(z) + np.abs(rest))).all(), np.max(off / (np.abs(z) + np.abs(rest)))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n, d, f, o", [(50, 40, 96, 24), (300, 130, 200, 70)])
+def test_gelu_gates_that_sit_negative(n, d, f, o, dtype):
+    # gates around -6 to -3: every H is a tail's
+    t, a = gated_inputs(n, d, f, o, dtype, True, 5 * n)
+    set_rows(t, a, "bg", slice(None), lambda x: torch.linspace(-6.0, -3.0, f).to(x))
+    set_rows(t, a, "Wg", slice(None), lambda x: x * 0.25)
+    a["bd"], a["R"] = np.zeros(o), np.zeros((n, o))
+    case(f"gated, negative gates {(n, d, f, o)} {dtype}")
+    w = [t[k] for k in WEIGHTS[:6]] + [None]
+    want = gated_results(a, "gelu", False)
+    Y, saved = fd.fd_gated_forward(*w, act="gelu", save=True)
+    g = fd.fd_gated_backward(t["dY"], *w, act="gelu", saved=saved)
+    for name in ("Y", "dX", "dWg", "dWu", "dWd", "dbg", "dbu"):
+        off = worst_lines(to_np(Y if name == "Y" else getattr(g, name)), *want[name])
+        assert max(off["row"], off["column"]) <= GATED_TOL[dtype], (name, off)
