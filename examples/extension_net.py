@@ -98,7 +98,9 @@ class ExtensionNet:
         off = Y.float() - target
         self.backward((off * (2.0 / off.numel())).to(self.dtype), tape)
         self.steps += 1
-        fd.fd_adamw_step(self.plan, self.steps, lr=lr, weight_decay=weight_decay)
+        # 8-bit moments: rounded to nearest, the second would stand still
+        fd.fd_adamw_step(self.plan, self.steps, lr=lr, weight_decay=weight_decay,
+                         rounding="unbiased")
         return off.square().mean()
 
 

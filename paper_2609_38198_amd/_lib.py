@@ -42,6 +42,7 @@ EXPORTS = (
     "fd_gated_forward", "fd_gated_backward", "fd_adamw_default_opts", "fd_adamw_step",
 )
 FD_ACT = {"silu": 0, "gelu": 1}
+FD_ROUNDING = {"nearest": 0, "unbiased": 1}
 FD_KERNEL_PRODUCT, FD_KERNEL_ROWSUM = 0, 1
 
 
@@ -116,7 +117,7 @@ class AdamwOpts(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
                 ("grad_scale", ctypes.c_double), ("step", ctypes.c_int64),
-                ("state_bits", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+                ("state_bits", ctypes.c_int32), ("rounding", ctypes.c_int32)]
 
 
 _c_i64 = ctypes.c_int64
@@ -890,7 +891,14 @@ def fd_adamw_plan(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
 
 def fd_adamw_step(plan: AdamwPlan, step: int, lr: float = 1e-3, beta1: float = 0.9,
                   beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
-                  grad_scale: float = 1.0) -> None:
-    """One AdamW step over the plan's tensors, in place; `step` counts from 1."""
-    o = AdamwOpts(lr, beta1, beta2, eps, weight_decay, grad_scale, step, plan.bits, 0)
+                  grad_scale: float = 1.0, rounding: str = "nearest") -> None:
+    """One AdamW step over the plan's tensors, in place; `step` counts from 1.
+
+    rounding, of 8-bit states: "nearest", or "unbiased" by a fixed hash of step and
+    element, with which the moments follow their formulas over many steps (rounded to
+    nearest, the second moment hardly moves)."""
+    if rounding not in FD_ROUNDING:
+        raise ValueError(f"rounding must be one of {sorted(FD_ROUNDING)}, got {rounding!r}")
+    o = AdamwOpts(lr, beta1, beta2, eps, weight_decay, grad_scale, step, plan.bits,
+                  FD_ROUNDING[rounding])
     _check(load().fd_adamw_step(plan.table, len(plan.table), o, _net_stream(plan.device)))

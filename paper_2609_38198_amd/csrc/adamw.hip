@@ -30,6 +30,7 @@ struct ScaledTensor : Tensor {  // of 8-bit states
 };
 struct Step {
   float b1, nb1, b2, nb2, rate, root, eps, gscale;
+  uint32_t seed;  // of unbiased rounding: the step's
 };
 // The tensors of a launch travel in its arguments, of which there are 4 KB: a launch
 // less is 5 to 7 us of a step (60 tensors, 14.9 million elements: 100 us in two, 92 in one).
@@ -128,10 +129,40 @@ __device__ __forceinline__ void widen_e4m3(int w, float scale, float* out) {
   out[3] = hi[1] * scale;
 }
 
-// Four values of a block whose largest finite magnitude is found over the wave;
-// returns the block's scale.
+// 32 well mixed bits of a number and a seed: every element and step has its own,
+// the same in every run.
+__host__ __device__ inline uint32_t mix(uint64_t at, uint32_t seed) {
+  uint32_t h = (uint32_t(at) * 0x9e3779b1u) ^ (uint32_t(at >> 32) * 0xddb3d743u) ^ seed;
+  h ^= h >> 16;
+  h *= 0xb504f333u;
+  h ^= h >> 15;
+  h *= 0xddb3d743u;
+  return h ^ (h >> 16);
+}
+
+// |y| <= 448 to one of the e4m3 values around it, up where `bits` as a fraction of one is
+// below the chance that makes the value's mean y; for a root, its square's mean y^2.
+// An e4m3 value is a float32 with 20 zero bits at the end, once 2^-6 is added to those below it.
 template <bool ROOT>
-__device__ __forceinline__ float narrow_e4m3(const float* x, unsigned char* q, int valid) {
+__device__ __forceinline__ float round_e4m3(float y, uint32_t bits) {
+  const float a = fabsf(y), shift = a < 0x1p-6f ? 0x1p-6f : 0.f;
+  const uint32_t w = __builtin_bit_cast(uint32_t, a + shift) & 0xfff00000u;
+  const float lo = __builtin_bit_cast(float, w) - shift;
+  const float hi = __builtin_bit_cast(float, w + 0x100000u) - shift;
+  float want = a - lo, gap = hi - lo;
+  if (ROOT) {
+    want *= a + lo;
+    gap *= hi + lo;
+  }
+  const float u = float(bits >> 8) * 0x1p-24f;
+  return copysignf(fminf(u * gap < want ? hi : lo, E4M3_TOP), y);
+}
+
+// Four values of a block whose largest finite magnitude is found over the wave;
+// returns the block's scale.  bits: four words for UNBIASED rounding.
+template <bool ROOT, bool UNBIASED>
+__device__ __forceinline__ float narrow_e4m3(const float* x, unsigned char* q, int valid,
+                                             const uint32_t* bits) {
 #pragma clang fp contract(off)
   float top = 0.f;
 #pragma unroll
@@ -147,6 +178,7 @@ __device__ __forceinline__ float narrow_e4m3(const float* x, unsigned char* q, i
   for (int i = 0; i < 4; ++i) {
     y[i] = x[i] * inv;
     if (ROOT && x[i] > 0.f && inv > 0.f) y[i] = fmaxf(y[i], E4M3_LEAST);
+    if (UNBIASED) y[i] = round_e4m3<ROOT>(y[i], bits[i]);
     if (!(fabsf(x[i]) < INFINITY)) y[i] = NAN;
   }
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
@@ -161,7 +193,9 @@ __device__ __forceinline__ float narrow_e4m3(const float* x, unsigned char* q, i
 
 // The 8-bit form: one wave takes the 256 elements that share a scale, so that
 // the new scale is a maximum over its lanes.  12 bytes an element, the gradient and the copy:
-// 152 million elements in 474 us, 5.1 TB/s.
+// 152 million elements in 468 us, 5.2 TB/s; with unbiased rounding, whose vector instructions
+// bound it, in 575.
+template <bool UNBIASED>
 __global__ __launch_bounds__(BLOCK) void adamw_e4m3_kernel(ScaledTable tb, Step s) {
   const int ti = find_tensor(tb, blockIdx.x);
   const ScaledTensor& t = tb.t[ti];
@@ -199,8 +233,15 @@ __global__ __launch_bounds__(BLOCK) void adamw_e4m3_kernel(ScaledTable tb, Step 
     }
     store_wide<4>(t.p + at, valid, p[j]);
     if (t.copy != nullptr) store_wide<4>(t.copy + at, valid, p[j]);
-    const float m1 = narrow_e4m3<false>(m, M + at, valid);
-    const float r1 = narrow_e4m3<true>(r, V + at, valid);
+    uint32_t mb[4], rb[4];
+    if (UNBIASED)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        mb[i] = mix(uint64_t(at + i), s.seed);
+        rb[i] = mix(mb[i], s.seed);
+      }
+    const float m1 = narrow_e4m3<false, UNBIASED>(m, M + at, valid, mb);
+    const float r1 = narrow_e4m3<true, UNBIASED>(r, V + at, valid, rb);
     if (lane == 0) {
       t.ms[block / BLOCK] = m1;
       t.vs[block / BLOCK] = r1;
@@ -291,6 +332,8 @@ fd_status fd_adamw_step(const fd_adamw_tensor* tensors, int64_t count, const fd_
                    std::isfinite(o.weight_decay) && std::isfinite(o.grad_scale),
                FD_ERR_INVALID_ARG, "lr, eps, weight_decay and grad_scale must be finite, eps >= 0");
     const bool narrow_states = o.state_bits == 8;
+    FD_REQUIRE(o.rounding == FD_ROUND_NEAREST || o.rounding == FD_ROUND_UNBIASED,
+               FD_ERR_INVALID_ARG, "unknown rounding");
     for (int64_t i = 0; i < count; ++i) {
       const fd_adamw_tensor& t = tensors[i];
       FD_REQUIRE(t.n >= 0 && t.n <= int64_t(1) << 40, FD_ERR_INVALID_ARG, "tensor size out of range");
@@ -316,9 +359,11 @@ fd_status fd_adamw_step(const fd_adamw_tensor* tensors, int64_t count, const fd_
     s.root = float(1.0 / std::sqrt(1.0 - std::pow(o.beta2, double(o.step))));
     s.eps = float(o.eps);
     s.gscale = float(o.grad_scale);
+    s.seed = mix(uint64_t(o.step), 0x6a09e667u);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (narrow_states)
-      run<ScaledTable>(adamw_e4m3_kernel, tensors, count, o, s, st);
+      run<ScaledTable>(o.rounding == FD_ROUND_UNBIASED ? adamw_e4m3_kernel<true> : adamw_e4m3_kernel<false>,
+                       tensors, count, o, s, st);
     else
       run<PlainTable>(adamw_kernel, tensors, count, o, s, st);
   });

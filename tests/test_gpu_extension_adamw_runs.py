@@ -1,0 +1,116 @@
+"""AdamW with 8-bit states over many steps."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import case, device, to_np
+from oracle import extension as ox
+from paper_2609_38198_amd import _lib as fd
+
+pytestmark = pytest.mark.gpu
+
+N, STEPS = 16384, 3000
+
+
+# The moments after 3,000 steps against their formulas in 64 bits, on every fourth element of
+# each block, whose gradients grew fourfold or ended at the first step.  With unbiased rounding v / (its
+# formula) has mean 1 and standard deviation 0.35 (0.7 where gradients ended): over 4,096
+# elements 0.011 at most, and 0.1 is nine of them.  Rounded to nearest, the roots' medians are
+# 0.43 and 4.4 times the formula's: that form is not meant for runs.
+@pytest.mark.parametrize("change", [4.0, 0.0])
+def test_moments_follow_their_formulas(change):
+    dev = device()
+    gen = torch.Generator(device=dev).manual_seed(5)
+
+    def normal():
+        return torch.randn(N, device=dev, generator=gen)
+
+    size = 0.1 * torch.exp(normal())
+    at = torch.arange(N, device=dev) % 4 == 1
+    p, g = torch.zeros(N, device=dev), torch.zeros(N, device=dev)
+    state = fd.fd_adamw_state([p], 8)
+    # start at the moments of the former gradients: one step with beta = 0
+    plan = fd.fd_adamw_plan([p], [g], state)
+    case(f"adamw 8-bit over {STEPS} steps, gradients times {change}")
+    g.copy_(size)
+    fd.fd_adamw_step(plan, 1, beta1=0.0, beta2=0.0, rounding="unbiased")
+
+    def wide(q, scale):
+        return q.double() * scale.double().repeat_interleave(256)
+
+    m, v = wide(state.m[0], state.m_scale[0]), wide(state.v[0], state.v_scale[0]).square()
+    grow = torch.where(at, change, 1.0)
+    for step in range(2, STEPS + 2):
+        g.copy_(normal() * size * grow)
+        fd.fd_adamw_step(plan, step, lr=1e-6, rounding="unbiased")
+        m = 0.9 * m + 0.1 * g.double()
+        v = 0.999 * v + 0.001 * g.double().square()
+    ratio = wide(state.v[0], state.v_scale[0]).square() / v
+    for part in (at, ~at):
+        assert abs(float(ratio[part].mean()) - 1.0) <= 0.1
+    root = ratio.sqrt()
+    assert 0.8 <= float(root[at].median()) <= 1.1 and 0.9 <= float(root[~at].median()) <= 1.1
+    # m: unbiased too, so the projection on the formula's is one (16,384 elements, noise 0.2 of m)
+    if change:
+        m8 = wide(state.m[0], state.m_scale[0]) / size.double()
+        m = m / size.double()
+        assert abs(float((m8 * m).sum() / (m * m).sum()) - 1.0) <= 0.05
+
+
+def test_one_unbiased_step():
+    # each code is one of the two around the value, the same in every call, another at
+    # another step; the scales and parameters are the other rounding's
+    rng = np.random.default_rng(7)
+    sizes, dev = [1, 255, 257, 4097, 10007], device()
+    ps = [torch.from_numpy(rng.normal(size=n)).float().to(dev) for n in sizes]
+    gs = [torch.from_numpy(rng.normal(size=n) * np.exp(2 * rng.normal(size=n))).float().to(dev)
+          for n in sizes]
+    table = ox.e4m3_values()
+    case("adamw, one unbiased step")
+    got = {}
+    for name, rounding, step in (("a", "unbiased", 7), ("b", "unbiased", 7), ("c", "unbiased", 8),
+                                 ("near", "nearest", 7)):
+        p = [x.clone() for x in ps]
+        st = fd.fd_adamw_state(p, 8)
+        plan = fd.fd_adamw_plan(p, gs, st)
+        fd.fd_adamw_step(plan, 1, beta1=0.0, beta2=0.0)  # moments of a size
+        before = [[to_np(x) for x in (m.float(), ms, r.float(), rs)]
+                  for m, ms, r, rs in zip(st.m, st.m_scale, st.v, st.v_scale)]
+        fd.fd_adamw_step(plan, step, rounding=rounding)
+        got[name] = p, st
+    differ = 0
+    for i, (m, ms, r, rs) in enumerate(before):
+        a, n = np.arange(sizes[i]) // 256, to_np(gs[i])
+        _, m1, v1 = ox.adamw(to_np(ps[i]), n, m * ms[a], (r * rs[a]) ** 2, 7, 1e-3)
+        assert torch.equal(got["a"][0][i], got["near"][0][i])
+        for field, x in (("m", m1), ("v", np.sqrt(v1))):
+            q = {k: getattr(s, field)[i].float() for k, (_, s) in got.items()}
+            scale = getattr(got["a"][1], field + "_scale")[i]
+            assert torch.equal(scale, getattr(got["near"][1], field + "_scale")[i])
+            assert torch.equal(q["a"], q["b"])
+            differ += int((q["a"] != q["c"]).sum())
+            y, code = np.abs(x) / to_np(scale)[a], np.abs(to_np(q["a"]))
+            # the codes around y; within the float32 roundings of one (8 x 2^-24) its far neighbour too
+            tol = 8 * 2.0 ** -24 * y
+            lo = table[np.clip(np.searchsorted(table, y - tol, side="right") - 1, 0, 126)]
+            hi = table[np.clip(np.searchsorted(table, y + tol, side="left"), 0, 126)]
+            least = 2.0 ** -9 if field == "v" else 0.0
+            assert ((code >= lo) & (code <= np.maximum(hi, least))).all(), (sizes[i], field)
+            assert (np.sign(to_np(q["a"])) * np.sign(x) >= 0).all()
+            if field == "v":
+                assert ((code > 0) == (x > 0)).all()
+    # m moves by a tenth of what rounding to nearest had left, 0.025 of a step on average, so that
+    # two steps' roundings differ in 2 x 0.025 of 14,617 values: 713, standard deviation 26
+    assert differ > 713 - 6 * 26
+
+
+def test_unbiased_not_finite_stays_alone():
+    dev = device()
+    p, g = torch.zeros(600, device=dev), torch.ones(600, device=dev)
+    g[300], g[5] = float("inf"), float("nan")
+    st = fd.fd_adamw_state([p], 8)
+    case("adamw, unbiased, with a NaN and an infinite gradient")
+    fd.fd_adamw_step(fd.fd_adamw_plan([p], [g], st), 1, rounding="unbiased")
+    for t in (p, st.m[0].float(), st.v[0].float()):
+        assert (~np.isfinite(to_np(t))).nonzero()[0].tolist() == [5, 300]
+    assert np.isfinite(to_np(st.m_scale[0])).all()
