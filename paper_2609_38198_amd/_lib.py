@@ -242,9 +242,12 @@ def _dtype_code(X: torch.Tensor) -> int:
 
 
 def _check_dev(*ts):
-    for t in ts:
-        if t is not None and not t.is_cuda:
-            raise ValueError("all tensors must live on the GPU")
+    """All tensors on one GPU (the workspace too: kernels write through its address)."""
+    ts = [t for t in ts if t is not None]
+    if any(not t.is_cuda for t in ts):
+        raise ValueError("all tensors must live on the GPU")
+    if len({t.get_device() for t in ts}) > 1:
+        raise ValueError("all tensors must live on the same GPU")
 
 
 def _workspace(nbytes: int, device) -> torch.Tensor:
@@ -288,7 +291,7 @@ def fd_kernel_matmul(Xr: torch.Tensor, Xc: Optional[torch.Tensor], beta: float, 
     lib = load()
     if Xc is None:
         Xc = Xr
-    _check_dev(Xr, Xc, V, sl, sr, Y)
+    _check_dev(Xr, Xc, V, sl, sr, Y, ws)
     if Xr.dim() != 2 or Xc.dim() != 2 or Xr.shape[1] != Xc.shape[1]:
         raise ValueError("Xr and Xc must be N x D with the same D")
     if Xr.stride(1) != 1 or Xc.stride(1) != 1 or Xr.stride(0) != Xc.stride(0):
@@ -367,7 +370,7 @@ def fd_degree(X: torch.Tensor, beta: float, alpha: float = 0.5,
               ws: Optional[torch.Tensor] = None) -> Degree:
     """q = K 1, d = w (K w) with w = q^-alpha, s = w d^-1/2, S_off = sum(q) - N."""
     lib = load()
-    _check_dev(X)
+    _check_dev(X, ws)
     if X.dim() != 2 or X.stride(1) != 1:
         raise ValueError("X must be row-major N x D")
     N, D = X.shape
@@ -391,7 +394,7 @@ def fd_degree_dyadic(X: torch.Tensor, beta0: float, nbeta: int, alpha: float = 0
                      ws: Optional[torch.Tensor] = None) -> Degree:
     """fd_degree at beta0 * 2^l for l < nbeta: q, d, s are nbeta x N, s_off nbeta."""
     lib = load()
-    _check_dev(X)
+    _check_dev(X, ws)
     if X.dim() != 2 or X.stride(1) != 1:
         raise ValueError("X must be row-major N x D")
     N, D = X.shape
@@ -427,7 +430,7 @@ def fd_block_lanczos(X: torch.Tensor, beta: float, k: int, b: int, alpha: float 
                      ws: Optional[torch.Tensor] = None, allow_not_converged: bool = False) -> Eigen:
     """Top-k eigenpairs of M = diag(s) K diag(s) (Perron pair included)."""
     lib = load()
-    _check_dev(X, V0)
+    _check_dev(X, V0, ws)
     N, D = X.shape
     dev = X.device
     o = opts if opts is not None else default_opts()
@@ -469,7 +472,7 @@ def fd_continuation(X: torch.Tensor, n_steps: Sequence[int], beta_steps: Sequenc
                     allow=(FD_OK,)) -> Ladder:
     """Warm-started ladder over prefixes X[:n_t] and bandwidths beta_t."""
     lib = load()
-    _check_dev(X, V0)
+    _check_dev(X, V0, ws)
     N, D = X.shape
     dev = X.device
     T = len(n_steps)
@@ -525,7 +528,7 @@ def fd_beta_flow(X: torch.Tensor, k: int, b: int, alpha: float = 0.5,
                  allow=(FD_OK,)) -> Flow:
     """Bandwidth selection by the beta-function flow; eigenpairs at beta_x."""
     lib = load()
-    _check_dev(X)
+    _check_dev(X, ws)
     N, D = X.shape
     dev = X.device
     fo = fopts if fopts is not None else flow_default_opts()
@@ -561,8 +564,8 @@ def fd_beta_flow_cascade(Xs: Sequence[torch.Tensor], k: int, b: int, alpha: floa
     Xs = list(Xs)
     if not 1 <= len(Xs) <= 4:
         raise ValueError("the cascade takes 1 to 4 levels")
+    _check_dev(*Xs, ws)
     for X in Xs:
-        _check_dev(X)
         if X.dim() != 2 or X.stride(1) != 1 or X.shape != Xs[0].shape:
             raise ValueError("every level must be the same row-major N x D points")
     N, D = Xs[0].shape
@@ -606,10 +609,21 @@ def _net_dtype(t: torch.Tensor, what: str) -> int:
     raise TypeError(f"{what} must be float32 or bfloat16, got {t.dtype}")
 
 
-def _net_matrix(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str) -> int:
-    """The leading dimension of a row-major rows x cols matrix."""
-    if not t.is_cuda:
+def _net_device(X: torch.Tensor) -> int:
+    if not X.is_cuda:
         raise ValueError("all tensors must live on the GPU")
+    return X.get_device()
+
+
+def _net_place(t: torch.Tensor, dev: int, what: str) -> None:
+    if t.get_device() != dev:
+        raise ValueError(f"{what} must live on the GPU of the other tensors")
+
+
+def _net_matrix(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, dev: int,
+                what: str) -> int:
+    """The leading dimension of a row-major rows x cols matrix."""
+    _net_place(t, dev, what)
     if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
         raise ValueError(f"{what} must be {rows} x {cols}, got {tuple(t.shape)}")
     if t.dtype != dtype:
@@ -624,26 +638,34 @@ def _net_matrix(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what:
     return max(ld, cols)
 
 
-def _net_vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str):
+def _net_vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, dev: int, what: str):
     if t is None:
         return None
-    if not t.is_cuda:
-        raise ValueError("all tensors must live on the GPU")
+    _net_place(t, dev, what)
     if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{what} must be {n} contiguous values of {dtype}")
     return t.data_ptr()
 
 
 def _net_workspace(ws: Optional[torch.Tensor], need: int, like: torch.Tensor) -> torch.Tensor:
-    if ws is not None and ws.numel() * ws.element_size() >= need:
-        return ws
+    if ws is not None:
+        _net_room(ws, like.get_device(), "ws")
+        if ws.numel() * ws.element_size() >= need:
+            return ws
     return like.new_empty(max(need, 1), dtype=torch.uint8)
 
 
-def _net_stream(device: torch.device) -> int:
+def _net_room(t: torch.Tensor, dev: int, what: str) -> None:
+    """A buffer that the kernels address by its start and its bytes."""
+    _net_place(t, dev, what)
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+
+
+def _net_stream(dev: int) -> int:
     # the current stream's handle without building a torch.cuda.Stream, which
     # takes 2 us of a call's 12
-    return torch._C._cuda_getCurrentRawStream(device.index)
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
 def fd_layer_norm(X: torch.Tensor, gamma: Optional[torch.Tensor] = None,
@@ -656,22 +678,23 @@ def fd_layer_norm(X: torch.Tensor, gamma: Optional[torch.Tensor] = None,
         raise ValueError("X must be N x D")
     N, D = X.shape
     xt = _net_dtype(X, "X")
-    ldx = _net_matrix(X, N, D, X.dtype, "X")
+    dev = _net_device(X)
+    ldx = _net_matrix(X, N, D, X.dtype, dev, "X")
     w = gamma if gamma is not None else beta
     wdtype = X.dtype if w is None else w.dtype
     wt = xt if w is None else _net_dtype(w, "gamma and beta")
-    pg = _net_vector(gamma, D, wdtype, "gamma")
-    pb = _net_vector(beta, D, wdtype, "beta")
+    pg = _net_vector(gamma, D, wdtype, dev, "gamma")
+    pb = _net_vector(beta, D, wdtype, dev, "beta")
     if Y is None:
         Y = X.new_empty((N, D))
     if stats is None:
         stats = X.new_empty((N, 2), dtype=torch.float32)
-    _net_matrix(stats, N, 2, torch.float32, "stats")
+    _net_matrix(stats, N, 2, torch.float32, dev, "stats")
     if not stats.is_contiguous():
         raise ValueError("stats must be contiguous")
-    _check(lib.fd_layer_norm(X.data_ptr(), xt, N, D, ldx, pg, pb, wt, eps, Y.data_ptr(),
-                             _net_matrix(Y, N, D, X.dtype, "Y"), stats.data_ptr(),
-                             _net_stream(X.device)))
+    ldy = _net_matrix(Y, N, D, X.dtype, dev, "Y")
+    _check(lib.fd_layer_norm(X.data_ptr(), xt, N, D, ldx, pg, pb, wt, eps, Y.data_ptr(), ldy,
+                             stats.data_ptr(), _net_stream(dev)))
     return Y, stats
 
 
@@ -694,25 +717,25 @@ def fd_layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[to
     if X.dim() != 2:
         raise ValueError("X must be N x D")
     N, D = X.shape
-    dev = X.device
     xt = _net_dtype(X, "X")
-    ldx = _net_matrix(X, N, D, X.dtype, "X")
-    lddy = _net_matrix(dY, N, D, X.dtype, "dY")
-    ldadd = 0 if add is None else _net_matrix(add, N, D, X.dtype, "add")
+    dev = _net_device(X)
+    ldx = _net_matrix(X, N, D, X.dtype, dev, "X")
+    lddy = _net_matrix(dY, N, D, X.dtype, dev, "dY")
+    ldadd = 0 if add is None else _net_matrix(add, N, D, X.dtype, dev, "add")
     wdtype = X.dtype if gamma is None else gamma.dtype
     wt = xt if gamma is None else _net_dtype(gamma, "gamma")
-    pg = _net_vector(gamma, D, wdtype, "gamma")
-    _net_matrix(stats, N, 2, torch.float32, "stats")
+    pg = _net_vector(gamma, D, wdtype, dev, "gamma")
+    _net_matrix(stats, N, 2, torch.float32, dev, "stats")
     if not stats.is_contiguous():
         raise ValueError("stats must be contiguous")
     if dX is None:
         dX = X.new_empty((N, D))
-    lddx = _net_matrix(dX, N, D, X.dtype, "dX")
+    lddx = _net_matrix(dX, N, D, X.dtype, dev, "dX")
     if weight_grads:
         dgamma = X.new_empty(D, dtype=wdtype) if dgamma is None else dgamma
         dbeta = X.new_empty(D, dtype=wdtype) if dbeta is None else dbeta
-    pdg = _net_vector(dgamma, D, wdtype, "dgamma")
-    pdb = _net_vector(dbeta, D, wdtype, "dbeta")
+    pdg = _net_vector(dgamma, D, wdtype, dev, "dgamma")
+    pdb = _net_vector(dbeta, D, wdtype, dev, "dbeta")
     ws = _net_workspace(ws, lib.fd_layer_norm_workspace_size(N, D), X)
     _check(lib.fd_layer_norm_backward(
         dY.data_ptr(), lddy, X.data_ptr(), xt, N, D, ldx, pg, wt, stats.data_ptr(),
@@ -730,14 +753,15 @@ def _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act) -> GatedBlock:
     F, O = Wg.shape[0], Wd.shape[0]
     t = X.dtype
     code = _net_dtype(X, "X")
-    ldx = _net_matrix(X, N, D, t, "X")
-    ldwi = _net_matrix(Wg, F, D, t, "Wg")
-    if _net_matrix(Wu, F, D, t, "Wu") != ldwi:
+    dev = _net_device(X)
+    ldx = _net_matrix(X, N, D, t, dev, "X")
+    ldwi = _net_matrix(Wg, F, D, t, dev, "Wg")
+    if _net_matrix(Wu, F, D, t, dev, "Wu") != ldwi:
         raise ValueError("Wg and Wu must have the same leading dimension")
-    ldwd = _net_matrix(Wd, O, F, t, "Wd")
+    ldwd = _net_matrix(Wd, O, F, t, dev, "Wd")
     return GatedBlock(N, D, F, O, code, FD_ACT[act], X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(),
-                      Wd.data_ptr(), _net_vector(bg, F, t, "bg"), _net_vector(bu, F, t, "bu"),
-                      _net_vector(bd, O, t, "bd"), ldx, ldwi, ldwd)
+                      Wd.data_ptr(), _net_vector(bg, F, t, dev, "bg"), _net_vector(bu, F, t, dev, "bu"),
+                      _net_vector(bd, O, t, dev, "bd"), ldx, ldwi, ldwd)
 
 
 def fd_gated_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor,
@@ -751,11 +775,11 @@ def fd_gated_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: to
     inner activations again."""
     lib = load()
     b = _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act)
-    dev = X.device
+    dev = X.get_device()
     if Y is None:
         Y = X.new_empty((b.N, b.O))
-    ldy = _net_matrix(Y, b.N, b.O, X.dtype, "Y")
-    ldr = 0 if R is None else _net_matrix(R, b.N, b.O, X.dtype, "R")
+    ldy = _net_matrix(Y, b.N, b.O, X.dtype, dev, "Y")
+    ldr = 0 if R is None else _net_matrix(R, b.N, b.O, X.dtype, dev, "R")
     saved, nsaved = None, 0
     if save:
         nsaved = lib.fd_gated_saved_size(b)
@@ -789,8 +813,8 @@ def fd_gated_backward(dY: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: t
     given; a bias has one where it was given."""
     lib = load()
     b = _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act)
-    dev, t = X.device, X.dtype
-    lddy = _net_matrix(dY, b.N, b.O, t, "dY")
+    dev, t = X.get_device(), X.dtype
+    lddy = _net_matrix(dY, b.N, b.O, t, dev, "dY")
     if grads is None:
         def like(x):
             return None if x is None else x.new_empty(x.shape)
@@ -798,14 +822,16 @@ def fd_gated_backward(dY: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: t
         grads = GatedGrads(like(X) if want_dx else None, like(Wg), like(Wu), like(Wd), like(bg),
                            like(bu), like(bd))
     g = grads
-    lddwi = _net_matrix(g.dWg, b.F, b.D, t, "dWg")
-    if _net_matrix(g.dWu, b.F, b.D, t, "dWu") != lddwi:
+    lddwi = _net_matrix(g.dWg, b.F, b.D, t, dev, "dWg")
+    if _net_matrix(g.dWu, b.F, b.D, t, dev, "dWu") != lddwi:
         raise ValueError("dWg and dWu must have the same leading dimension")
     c = GatedGradsC(None if g.dX is None else g.dX.data_ptr(), g.dWg.data_ptr(),
-                    g.dWu.data_ptr(), g.dWd.data_ptr(), _net_vector(g.dbg, b.F, t, "dbg"),
-                    _net_vector(g.dbu, b.F, t, "dbu"), _net_vector(g.dbd, b.O, t, "dbd"),
-                    0 if g.dX is None else _net_matrix(g.dX, b.N, b.D, t, "dX"), lddwi,
-                    _net_matrix(g.dWd, b.O, b.F, t, "dWd"))
+                    g.dWu.data_ptr(), g.dWd.data_ptr(), _net_vector(g.dbg, b.F, t, dev, "dbg"),
+                    _net_vector(g.dbu, b.F, t, dev, "dbu"), _net_vector(g.dbd, b.O, t, dev, "dbd"),
+                    0 if g.dX is None else _net_matrix(g.dX, b.N, b.D, t, dev, "dX"), lddwi,
+                    _net_matrix(g.dWd, b.O, b.F, t, dev, "dWd"))
+    if saved is not None:
+        _net_room(saved, dev, "saved")
     nsaved = 0 if saved is None else saved.numel() * saved.element_size()
     need = lib.fd_gated_workspace_size(b, 2 if saved is None else 1)
     ws = _net_workspace(ws, need, X)
@@ -863,13 +889,13 @@ def fd_adamw_plan(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
     if any(len(x) != n for x in lists) or (decay is not None and len(decay) != n):
         raise ValueError("one tensor for each parameter is wanted")
     moment = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    dev = _net_device(params[0]) if n else -1
     table = (AdamwTensor * n)()
     for i, p in enumerate(params):
         size = p.numel()
 
         def at(t, dtypes, what, count=size):
-            if not t.is_cuda:
-                raise ValueError("all tensors must live on the GPU")
+            _net_place(t, dev, f"{what} of tensor {i}")
             if t.numel() != count or t.dtype not in dtypes or not t.is_contiguous():
                 raise ValueError(f"{what} of tensor {i} must be {count} contiguous values of "
                                  f"{' or '.join(map(str, dtypes))}")
@@ -901,4 +927,4 @@ def fd_adamw_step(plan: AdamwPlan, step: int, lr: float = 1e-3, beta1: float = 0
         raise ValueError(f"rounding must be one of {sorted(FD_ROUNDING)}, got {rounding!r}")
     o = AdamwOpts(lr, beta1, beta2, eps, weight_decay, grad_scale, step, plan.bits,
                   FD_ROUNDING[rounding])
-    _check(load().fd_adamw_step(plan.table, len(plan.table), o, _net_stream(plan.device)))
+    _check(load().fd_adamw_step(plan.table, len(plan.table), o, _net_stream(plan.device.index)))

@@ -1,5 +1,7 @@
 """More of what the extension's entry points and their binding refuse (no GPU needed)."""
+import numpy as np
 import pytest
+import torch
 
 from paper_2609_38198_amd import _lib as fd
 
@@ -16,3 +18,81 @@ def test_adamw_refuses_an_unknown_rounding():
     assert o.rounding == fd.FD_ROUNDING["nearest"] == 0
     with pytest.raises(ValueError):
         fd.fd_adamw_step(None, 1, rounding="up")
+
+
+class Elsewhere:
+    """Looks like a torch tensor on GPU `dev` (-1: in host memory) to the binding, which
+    refuses it before it would use its address."""
+
+    def __init__(self, *shape, dtype=torch.float32, dev=0, strides=None):
+        self.shape, self.dtype, self.dev = tuple(shape), dtype, dev
+        self.strides = strides or tuple(int(np.prod(shape[i + 1:])) for i in range(len(shape)))
+
+    is_cuda = property(lambda self: self.dev >= 0)
+    device = property(lambda self: torch.device("cuda", self.dev) if self.dev >= 0 else torch.device("cpu"))
+
+    def get_device(self):
+        return self.dev
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self, i=None):
+        return self.strides if i is None else self.strides[i]
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def is_contiguous(self):
+        return self.strides == Elsewhere(*self.shape).strides
+
+    def data_ptr(self):
+        raise AssertionError("the address of a tensor that had to be refused")
+
+    def new_empty(self, shape, dtype=None):
+        return type(self)(*(shape if isinstance(shape, (tuple, list)) else (shape,)),
+                          dtype=dtype or self.dtype, dev=self.dev)
+
+
+class Here(Elsewhere):
+    def data_ptr(self):
+        return 256
+
+
+@pytest.mark.parametrize("dev", [-1, 1])
+def test_binding_refuses_tensors_of_another_device(dev):
+    x, w, wd, v = Here(4, 8), Here(16, 8), Here(8, 16), Here(8)
+    ms = Here(4, 2)
+
+    def away(*shape, dtype=torch.float32):
+        return Elsewhere(*shape, dtype=dtype, dev=dev)
+
+    room = away(1 << 24, dtype=torch.uint8)
+    apart = Elsewhere(1 << 12, 64, dtype=torch.uint8, strides=(128, 1))
+    calls = [lambda: fd.fd_layer_norm(x, away(8)), lambda: fd.fd_layer_norm(x, v, away(8)),
+             lambda: fd.fd_layer_norm(x, Y=away(4, 8)), lambda: fd.fd_layer_norm(x, stats=away(4, 2)),
+             lambda: fd.fd_layer_norm_backward(x, x, v, away(4, 2)),
+             lambda: fd.fd_layer_norm_backward(away(4, 8), x, v, ms),
+             lambda: fd.fd_layer_norm_backward(x, x, v, ms, ws=room),
+             lambda: fd.fd_layer_norm_backward(x, x, v, ms, dgamma=away(8)),
+             lambda: fd.fd_gated_forward(x, w, away(16, 8), wd),
+             lambda: fd.fd_gated_forward(x, w, w, wd, R=away(4, 8)),
+             lambda: fd.fd_gated_forward(x, w, w, wd, ws=room),
+             lambda: fd.fd_gated_forward(x, w, w, wd, ws=apart),
+             lambda: fd.fd_gated_backward(x, x, w, w, wd, saved=room),
+             lambda: fd.fd_gated_backward(x, x, w, w, wd, saved=apart),
+             lambda: fd.fd_gated_backward(x, x, w, w, wd, ws=room),
+             lambda: fd.fd_kernel_matmul(x, None, 1.0, Here(4, 2), ws=room),
+             lambda: fd.fd_kernel_matmul(x, None, 1.0, away(4, 2)),
+             lambda: fd.fd_degree(x, 1.0, ws=room)]
+    state = fd.AdamwState([Here(8)], [Here(8)])
+    calls += [lambda: fd.fd_adamw_plan([v], [away(8)], state),
+              lambda: fd.fd_adamw_plan([v], [v], fd.AdamwState([away(8)], [v])),
+              lambda: fd.fd_adamw_plan([v, away(8)], [v, v], fd.AdamwState([v, v], [v, v]))]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError, match="GPU|contiguous"):
+            call()
+            raise AssertionError(f"call {i} was taken")

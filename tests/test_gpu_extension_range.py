@@ -118,3 +118,19 @@ def test_gelu_gates_that_sit_negative(n, d, f, o, dtype):
     for name in ("Y", "dX", "dWg", "dWu", "dWd", "dbg", "dbu"):
         off = worst_lines(to_np(Y if name == "Y" else getattr(g, name)), *want[name])
         assert max(off["row"], off["column"]) <= GATED_TOL[dtype], (name, off)
+
+
+def test_host_workspaces_are_refused():
+    t, _ = gated_inputs(40, 24, 48, 16, F32, False, 1)
+    w = [t[k] for k in WEIGHTS[:4]]
+    room = torch.empty(1 << 24, dtype=torch.uint8)
+    case("host workspaces")
+    Y, saved = fd.fd_gated_forward(*w, save=True)
+    _, stats = fd.fd_layer_norm(t["X"])
+    for call in (lambda: fd.fd_gated_forward(*w, ws=room),
+                 lambda: fd.fd_gated_backward(t["dY"], *w, ws=room),
+                 lambda: fd.fd_gated_backward(t["dY"], *w, saved=saved.cpu()),
+                 lambda: fd.fd_layer_norm_backward(t["X"], t["X"], None, stats, ws=room),
+                 lambda: fd.fd_kernel_matmul(t["X"], None, 1.0, t["X"], ws=room)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
