@@ -466,7 +466,7 @@ typedef struct fd_adamw_tensor {
   float* m_scale;    /* 8-bit states: a scale for each 256 elements (the last may be fewer) */
   float* v_scale;
   void* copy;        /* bfloat16 copy of the updated parameters, or NULL */
-  int64_t n;         /* >= 0 */
+  int64_t n;         /* 0 .. 2^35 */
   int32_t gt;        /* fd_dtype of g */
   float decay;       /* multiplies the step's weight decay (0: none) */
 } fd_adamw_tensor;

@@ -11,6 +11,7 @@ namespace {
 
 constexpr int BLOCK = 256;      // elements that share a scale, and threads of a workgroup
 constexpr int CHUNK = 4096;     // elements of a workgroup
+constexpr int64_t MAX_GROUPS = int64_t(1) << 23;  // workgroups of a launch
 constexpr float E4M3_TOP = 448.f;
 constexpr float E4M3_LEAST = 0x1p-9f;
 constexpr float LEAST_TOP = 0x1p-100f;  // a block below this is stored as zeros
@@ -255,11 +256,10 @@ void set_scales(ScaledTensor& d, const fd_adamw_tensor& t) {
   d.vs = t.v_scale;
 }
 
-// A launch for each table of tensors, or 2^30 workgroups.
+// A launch for each table of tensors, or 2^23 workgroups (2^31 threads).
 template <class TB>
 void run(void (*kernel)(TB, Step), const fd_adamw_tensor* tensors, int64_t count,
          const fd_adamw_opts& o, const Step& s, hipStream_t st) {
-  constexpr int64_t MAX_GROUPS = int64_t(1) << 30;
   constexpr int ROOM = int(sizeof(TB::t) / sizeof(TB::t[0]));
   TB tb{};
   int64_t groups = 0;
@@ -336,7 +336,7 @@ fd_status fd_adamw_step(const fd_adamw_tensor* tensors, int64_t count, const fd_
                FD_ERR_INVALID_ARG, "unknown rounding");
     for (int64_t i = 0; i < count; ++i) {
       const fd_adamw_tensor& t = tensors[i];
-      FD_REQUIRE(t.n >= 0 && t.n <= int64_t(1) << 40, FD_ERR_INVALID_ARG, "tensor size out of range");
+      FD_REQUIRE(t.n >= 0 && t.n <= MAX_GROUPS * CHUNK, FD_ERR_INVALID_ARG, "tensor size out of range");
       if (t.n == 0) continue;
       check_dtype(t.gt, "gradient dtype");
       FD_REQUIRE(t.p != nullptr && t.g != nullptr && t.m != nullptr && t.v != nullptr,

@@ -64,15 +64,16 @@ __device__ void column_sums(const PackJobs& jobs, int64_t id) {
 }
 
 template <class T>
-__global__ __launch_bounds__(GROUP) void before_kernel(PackJobs jobs) {
-  if (int64_t(blockIdx.x) >= jobs.groups) {
-    column_sums<T>(jobs, int64_t(blockIdx.x) - jobs.groups);
+__global__ __launch_bounds__(GROUP) void before_kernel(PackJobs jobs, int64_t first) {
+  const int64_t id = first + blockIdx.x;
+  if (id >= jobs.groups) {
+    column_sums<T>(jobs, id - jobs.groups);
     return;
   }
   int i = 0;
-  while (i + 1 < jobs.count && jobs.j[i + 1].first <= int64_t(blockIdx.x)) ++i;
+  while (i + 1 < jobs.count && jobs.j[i + 1].first <= id) ++i;
   const PackJob& job = jobs.j[i];
-  const int64_t at = (int64_t(blockIdx.x) - job.first) * GROUP + threadIdx.x;
+  const int64_t at = (id - job.first) * GROUP + threadIdx.x;
   const int64_t per = job.ldp / 8, row = at / per, col = (at - row * per) * 8;
   if (row >= job.rows) return;
   float x[8];
@@ -171,8 +172,9 @@ __global__ __launch_bounds__(GROUP) void after_kernel(AfterJobs jobs) {
 // Zero rows: weights' gradients are zero.
 template <class T>
 __global__ __launch_bounds__(GROUP) void clear_kernel(T* p, int64_t rows, int64_t cols, int64_t ld) {
-  const int64_t at = int64_t(blockIdx.x) * GROUP + threadIdx.x;
-  if (at < rows * cols) p[at / cols * ld + at % cols] = narrow<T>(0.f);
+  for (int64_t at = int64_t(blockIdx.x) * GROUP + threadIdx.x; at < rows * cols;
+       at += int64_t(gridDim.x) * GROUP)
+    p[at / cols * ld + at % cols] = narrow<T>(0.f);
 }
 
 // ---------------------------------------------------------------- products
@@ -284,10 +286,6 @@ int plan(Shape* s, int count, bool fine, int epilogue, bool columns) {
   return config;
 }
 
-void check_grid(int64_t groups) {
-  FD_REQUIRE(groups < (int64_t(1) << 31), FD_ERR_UNSUPPORTED, "problem too large for one launch");
-}
-
 template <class K>
 void allow_lds(K kernel, size_t bytes) {
   FD_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
@@ -302,11 +300,12 @@ void launch_config(GemmArgs& p, hipStream_t stream) {
   p.tiles_m = ceil_div(p.M, K::bm);
   // GATE and GRAD write whole padded rows
   p.tiles_n = ceil_div(EPI == STORE ? p.N : p.Fp, EPI == GATE ? K::bn / 2 : K::bn);
+  const int64_t groups = p.tiles_m * p.tiles_n * p.splits;
+  constexpr int THREADS = K::wm * K::wn * WAVE;
+  check_launch(groups, THREADS);
   auto kernel = gemm_kernel<K::bm, K::bn, K::wm, K::wn, ACOL, BCOL, EPI, T, ACT, PLA, PL, HP>;
   allow_lds(kernel, lds);
-  check_grid(p.tiles_m * p.tiles_n * p.splits);
-  kernel<<<dim3(unsigned(p.tiles_m * p.tiles_n * p.splits)), dim3(K::wm * K::wn * WAVE), lds,
-           stream>>>(p);
+  kernel<<<dim3(unsigned(groups)), dim3(THREADS), lds, stream>>>(p);
   FD_LAUNCH_CHECK();
 }
 
@@ -327,7 +326,7 @@ void launch_inner(int config, const Shape& s, float* part, GemmArgs& p, hipStrea
   launch<false, BCOL, EPI, T, ACT, HP>(config, p, stream);
   if (s.splits == 1) return;
   const int64_t groups = ceil_div(ceil_div(p.M, 32) * (p.Fp / 32), GROUP / WAVE);
-  check_grid(groups);
+  check_launch(groups, GROUP);
   finish_kernel<EPI, T, ACT, HP><<<dim3(unsigned(groups)), dim3(GROUP), 0, stream>>>(p);
   FD_LAUNCH_CHECK();
 }
@@ -346,10 +345,11 @@ void launch_group(GemmGroup& s, hipStream_t stream) {
     at += p.tiles_m * p.tiles_n * p.splits;
   }
   s.first[s.count] = at;
-  check_grid(at);
+  constexpr int THREADS = K::wm * K::wn * WAVE;
+  check_launch(at, THREADS);
   auto kernel = gemm_group_kernel<K::bm, K::bn, K::wm, K::wn, T, HP>;
   allow_lds(kernel, lds);
-  kernel<<<dim3(unsigned(at)), dim3(K::wm * K::wn * WAVE), lds, stream>>>(s);
+  kernel<<<dim3(unsigned(at)), dim3(THREADS), lds, stream>>>(s);
   FD_LAUNCH_CHECK();
 }
 
@@ -373,7 +373,7 @@ void add_columns(AfterJobs& after, const float* part, int64_t rows, int64_t ld, 
 template <class T>
 void run_after(const AfterJobs& after, hipStream_t stream) {
   if (after.groups == 0) return;
-  check_grid(after.groups);
+  check_launch(after.groups, GROUP);
   after_kernel<T><<<dim3(unsigned(after.groups)), dim3(GROUP), 0, stream>>>(after);
   FD_LAUNCH_CHECK();
 }
@@ -511,9 +511,12 @@ void run_before(const PackJobs& jobs, hipStream_t stream) {
   const int64_t sums = jobs.sum == nullptr ? 0 : ceil_div(jobs.sum_cols, WAVE) * jobs.sum_parts;
   const int64_t groups = jobs.groups + sums;
   if (groups == 0) return;
-  check_grid(groups);
-  before_kernel<T><<<dim3(unsigned(groups)), dim3(GROUP), 0, stream>>>(jobs);
-  FD_LAUNCH_CHECK();
+  // half a launch's threads at a time: packs of 2^35 elements and more fit the memory
+  constexpr int64_t SLICE = (int64_t(1) << 31) / GROUP;
+  for (int64_t first = 0; first < groups; first += SLICE) {
+    before_kernel<T><<<dim3(unsigned(std::min(SLICE, groups - first))), dim3(GROUP), 0, stream>>>(jobs, first);
+    FD_LAUNCH_CHECK();
+  }
 }
 
 // Operand rows (columns where `col`) of a matrix.
@@ -657,8 +660,7 @@ void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void*
 template <class T>
 void clear(void* p, int64_t rows, int64_t cols, int64_t ld, hipStream_t st) {
   if (p == nullptr) return;
-  const int64_t groups = ceil_div(rows * cols, GROUP);
-  check_grid(groups);
+  const int64_t groups = std::min<int64_t>(ceil_div(rows * cols, GROUP), 1 << 16);
   clear_kernel<T><<<dim3(unsigned(groups)), dim3(GROUP), 0, st>>>(static_cast<T*>(p), rows, cols, ld);
   FD_LAUNCH_CHECK();
 }

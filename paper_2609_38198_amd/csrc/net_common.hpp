@@ -82,6 +82,13 @@ __device__ __forceinline__ float wave_max(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(bits(), WAVE - 1));
 }
 
+// A launch holds fewer than 2^32 threads; one of more runs what is left over them
+// alone, without an error.
+inline void check_launch(int64_t groups, int64_t threads) {
+  FD_REQUIRE(groups < (int64_t(1) << 32) / threads, FD_ERR_UNSUPPORTED,
+             "problem too large for one launch");
+}
+
 // Checks shared by the entry points.
 inline void check_dtype(int t, const char* what) {
   FD_REQUIRE(t == FD_F32 || t == FD_BF16, FD_ERR_INVALID_ARG, std::string("unknown ") + what);

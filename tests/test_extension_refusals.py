@@ -96,3 +96,14 @@ def test_binding_refuses_tensors_of_another_device(dev):
         with pytest.raises(ValueError, match="GPU|contiguous"):
             call()
             raise AssertionError(f"call {i} was taken")
+
+
+def test_more_than_a_launch_holds_is_refused():
+    # 2^32 threads: beyond, a launch would run the rest alone and report nothing
+    lib = fd.load()
+    b = fd.GatedBlock(N=1 << 30, D=72, F=1024, O=72, type=1, act=0, X=256, Wg=256, Wu=256, Wd=256,
+                      ldx=72, ldwi=72, ldwd=1024)
+    assert lib.fd_gated_forward(b, None, 0, 256, 72, None, 0, 256, 1 << 62, None) == 2
+    assert b"launch" in lib.fd_last_error()
+    t = fd.AdamwTensor(p=256, g=256, m=256, v=256, n=(1 << 35) + 1, gt=0, decay=1.0)
+    assert lib.fd_adamw_step(t, 1, None, None) == 1

@@ -134,3 +134,32 @@ def test_host_workspaces_are_refused():
                  lambda: fd.fd_kernel_matmul(t["X"], None, 1.0, t["X"], ws=room)):
         with pytest.raises(ValueError, match="GPU"):
             call()
+
+
+def test_packs_of_more_threads_than_a_launch_holds():
+    # 480 million rows of 65 bfloat16 features (62 GB) are packed by 4.32e9 threads; rows all over
+    # it, against the same rows by themselves
+    n, d, f = 480_000_000, 65, 16
+    dev = device()
+    need = 2 * n * (d + 72 + 64 + 2) + (1 << 32)
+    if torch.cuda.mem_get_info()[0] < need:
+        pytest.skip("needs 200 GB of GPU memory")
+    case(f"gated {n} x {d} -> {f} -> 1")
+    gen = torch.Generator(device=dev).manual_seed(3)
+
+    def normal(*shape):
+        return torch.randn(*shape, device=dev, generator=gen).to(BF16)
+
+    X = torch.zeros(n, d, dtype=BF16, device=dev)
+    at = torch.cat([torch.arange(40, device=dev), torch.arange(1, 200, device=dev) * (n // 200) + 17,
+                    n - 1 - torch.arange(40, device=dev)])
+    X[at] = normal(len(at), d)
+    w = [normal(f, d) * 0.1, normal(f, d) * 0.1, normal(1, f), normal(f), normal(f)]
+    Y, _ = fd.fd_gated_forward(X, *w)
+    few, _ = fd.fd_gated_forward(X[at].contiguous(), *w)
+    # H in one plane and in two: two bfloat16 roundings apart at most, of the sum's terms
+    got, want = to_np(Y[at]), to_np(few)
+    del X, Y
+    torch.cuda.empty_cache()
+    assert np.linalg.norm(got - want) <= 2.0 ** -7 * np.linalg.norm(want)
+    assert np.abs(got - want).max() <= 2.0 ** -6 * np.abs(want).max()
