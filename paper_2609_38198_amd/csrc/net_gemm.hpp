@@ -38,18 +38,21 @@ struct Operand {
 // wait for every such load before any LDS read; the write to M0 needs one
 // wait state before its use.  From each lane's byte offset to a uniform base, or from each
 // lane's own address.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // M0 is written and said to be
 __device__ __forceinline__ void lds_load16(const char* base, uint32_t off, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
                : "s"(to), "v"(off), "s"(base)
-               : "memory");
+               : "memory", "m0");
 }
 __device__ __forceinline__ void lds_load16(const void* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :
                : "s"(to), "v"(from)
-               : "memory");
+               : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // A value that is the same in every lane, in a scalar register.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }

@@ -107,3 +107,19 @@ def test_more_than_a_launch_holds_is_refused():
     assert b"launch" in lib.fd_last_error()
     t = fd.AdamwTensor(p=256, g=256, m=256, v=256, n=(1 << 35) + 1, gt=0, decay=1.0)
     assert lib.fd_adamw_step(t, 1, None, None) == 1
+
+
+def test_assembly_names_the_registers_that_it_writes():
+    # a statement that writes M0 without saying so is right until the compiler keeps something there
+    import glob
+    import os
+    import re
+
+    csrc = os.path.join(os.path.dirname(fd.__file__), "csrc")
+    found = 0
+    for path in glob.glob(os.path.join(csrc, "*.h*")):
+        for text in re.findall(r"asm volatile\((.*?)\);", open(path).read(), re.S):
+            if re.search(r"\bm0,", text.split(":")[0]):
+                found += 1
+                assert '"m0"' in text.split(":")[-1], path
+    assert found
