@@ -601,12 +601,16 @@ def fd_beta_flow_cascade(Xs: Sequence[torch.Tensor], k: int, b: int, alpha: floa
 # ---- a parametric extension of the coordinates ----
 
 
-def _net_dtype(t: torch.Tensor, what: str) -> int:
-    if t.dtype == torch.float32:
+def _net_code(dtype: torch.dtype, what: str) -> int:
+    if dtype == torch.float32:
         return FD_F32
-    if t.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return FD_BF16
-    raise TypeError(f"{what} must be float32 or bfloat16, got {t.dtype}")
+    raise TypeError(f"{what} must be float32 or bfloat16, got {dtype}")
+
+
+def _net_dtype(t: torch.Tensor, what: str) -> int:
+    return _net_code(t.dtype, what)
 
 
 def _net_device(X: torch.Tensor) -> int:
@@ -710,9 +714,11 @@ def fd_layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[to
                            weight_grads: bool = True, dX: Optional[torch.Tensor] = None,
                            dgamma: Optional[torch.Tensor] = None,
                            dbeta: Optional[torch.Tensor] = None,
-                           ws: Optional[torch.Tensor] = None) -> LayerNormGrads:
+                           ws: Optional[torch.Tensor] = None,
+                           wdtype: Optional[torch.dtype] = None) -> LayerNormGrads:
     """Gradients of fd_layer_norm, into dX, dgamma and dbeta where given; `add`, a
-    residual branch's gradient, is added to dX."""
+    residual branch's gradient, is added to dX.  dgamma and dbeta have gamma's type; without
+    gamma, that of the array given for one of them, or wdtype, or X's."""
     lib = load()
     if X.dim() != 2:
         raise ValueError("X must be N x D")
@@ -722,8 +728,10 @@ def fd_layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[to
     ldx = _net_matrix(X, N, D, X.dtype, dev, "X")
     lddy = _net_matrix(dY, N, D, X.dtype, dev, "dY")
     ldadd = 0 if add is None else _net_matrix(add, N, D, X.dtype, dev, "add")
-    wdtype = X.dtype if gamma is None else gamma.dtype
-    wt = xt if gamma is None else _net_dtype(gamma, "gamma")
+    given = [w.dtype for w in (gamma, dgamma, dbeta) if w is not None]
+    if wdtype is None:
+        wdtype = given[0] if given else X.dtype
+    wt = _net_code(wdtype, "gamma, dgamma and dbeta")
     pg = _net_vector(gamma, D, wdtype, dev, "gamma")
     _net_matrix(stats, N, 2, torch.float32, dev, "stats")
     if not stats.is_contiguous():

@@ -123,3 +123,15 @@ def test_assembly_names_the_registers_that_it_writes():
                 found += 1
                 assert '"m0"' in text.split(":")[-1], path
     assert found
+
+
+def test_layer_norm_gradients_types():
+    x, v, ms = Here(4, 8, dtype=torch.bfloat16), Here(8, dtype=torch.float32), Here(4, 2)
+    half = Here(8, dtype=torch.float16)
+    for kw in (dict(gamma=v, dbeta=Here(8, dtype=torch.bfloat16)), dict(gamma=v, wdtype=torch.bfloat16),
+               dict(gamma=None, dgamma=v, dbeta=Here(8, dtype=torch.bfloat16))):
+        with pytest.raises(ValueError):
+            fd.fd_layer_norm_backward(x, x, stats=ms, **kw)
+    for kw in (dict(gamma=half), dict(gamma=None, dbeta=half), dict(gamma=None, wdtype=torch.float64)):
+        with pytest.raises(TypeError):
+            fd.fd_layer_norm_backward(x, x, stats=ms, **kw)
