@@ -639,7 +639,7 @@ def _net_matrix(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, dev: 
         if ld < cols:
             raise ValueError(f"{what} has overlapping rows")
         return ld
-    return max(ld, cols)
+    return cols  # of one row whatever its stride says
 
 
 def _net_vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, dev: int, what: str):
