@@ -1,6 +1,7 @@
 // AdamW over many tensors in few launches, states in 32 or 8 bits.
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "fd_guard.hpp"
 #include "net_common.hpp"
@@ -357,7 +358,8 @@ fd_status fd_adamw_step(const fd_adamw_tensor* tensors, int64_t count, const fd_
     s.nb2 = float(1.0 - o.beta2);
     s.rate = float(o.lr / (1.0 - std::pow(o.beta1, double(o.step))));
     s.root = float(1.0 / std::sqrt(1.0 - std::pow(o.beta2, double(o.step))));
-    s.eps = float(o.eps);
+    // an eps that float32 would round to zero still keeps 0 / (0 + eps) at zero
+    s.eps = o.eps > 0 ? std::max(float(o.eps), std::numeric_limits<float>::min()) : 0.f;
     s.gscale = float(o.grad_scale);
     s.seed = mix(uint64_t(o.step), 0x6a09e667u);
     hipStream_t st = static_cast<hipStream_t>(stream);

@@ -114,3 +114,16 @@ def test_unbiased_not_finite_stays_alone():
     for t in (p, st.m[0].float(), st.v[0].float()):
         assert (~np.isfinite(to_np(t))).nonzero()[0].tolist() == [5, 300]
     assert np.isfinite(to_np(st.m_scale[0])).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_an_eps_below_float32(bits):
+    dev = device()
+    p, g = torch.full((300,), 2.0, device=dev), torch.zeros(300, device=dev)
+    g[7] = 1.0
+    st = fd.fd_adamw_state([p], bits)
+    case(f"adamw, eps 1e-60, {bits}-bit states")
+    fd.fd_adamw_step(fd.fd_adamw_plan([p], [g], st), 1, lr=0.125, eps=1e-60, weight_decay=0.0)
+    want = np.full(300, 2.0)
+    want[7] -= 0.125
+    assert np.abs(to_np(p) - want).max() <= 16 * 2.0 ** -24
