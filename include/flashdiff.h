@@ -374,7 +374,7 @@ fd_status fd_beta_flow_cascade(const void* const* Xs, const fd_dtype* xts, const
  *    16 bytes are the fast case.  N = 0 rows are allowed: nothing is written but the
  *    gradients of weights and biases, which are then zero.
  *  - FD_F32 computes to float32 accuracy; FD_BF16 accumulates in float32 and
- *    rounds each stored value once.
+ *    rounds each output once (and the gated block's inner values, see FD_GATED_FINE).
  *  - Non-finite inputs are not refused: they come out as NaN or infinity where the
  *    formulas let them through, and rows that do not meet them stay clean. */
 
@@ -408,12 +408,21 @@ typedef enum fd_activation {
   FD_ACT_GELU = 1  /* g (1 + erf(g / sqrt 2)) / 2 */
 } fd_activation;
 
+/* Or-ed to fd_gated_block.act, for FD_BF16.  The block's inner values H, dG and dU
+ * are operands of its second products.  Where N F max(D, O) <= 2^25 they are held in two
+ * bfloat16 values each (16 bits or more), and Y and the gradients are off by the rounding of their own storage.
+ * Above it they are rounded to one bfloat16 value, as large, which makes the results' error
+ * 1.4 times that; so a row's last bits may differ between a small and a large call.  With this
+ * flag they take two at all sizes, in 1.5 times the time at 5003 x 509 -> 1365 -> 509 and
+ * 3.2 times at 16384 x 2048 -> 8192 -> 2048. */
+enum { FD_GATED_FINE = 0x100 };
+
 /* Gated feed-forward block D -> F -> O:
  *     G = X Wg^T + bg,  U = X Wu^T + bu,  H = act(G) * U,  Y = H Wd^T + bd [+ R]. */
 typedef struct fd_gated_block {
   int64_t N, D, F, O;   /* rows; input, inner and output widths */
   int32_t type;         /* fd_dtype of X, the weights, the biases, Y and all gradients */
-  int32_t act;          /* fd_activation */
+  int32_t act;          /* fd_activation, and FD_GATED_FINE where wanted */
   const void* X;        /* N x D */
   const void *Wg, *Wu;  /* F x D each */
   const void* Wd;       /* O x F */
@@ -438,7 +447,7 @@ size_t fd_gated_saved_size(const fd_gated_block* b);
 
 /* Bytes of workspace of fd_gated_forward (backward = 0) or fd_gated_backward
  * (1: with saved, 2: without), whatever the alignments.  0 for sizes that they reject; only
- * N, D, F, O and type are read. */
+ * N, D, F, O, type and act's FD_GATED_FINE are read. */
 size_t fd_gated_workspace_size(const fd_gated_block* b, int32_t backward);
 
 /* Y (N x O), with R (N x O or NULL) added; Y may be R with the same leading

@@ -42,6 +42,7 @@ EXPORTS = (
     "fd_gated_forward", "fd_gated_backward", "fd_adamw_default_opts", "fd_adamw_step",
 )
 FD_ACT = {"silu": 0, "gelu": 1}
+FD_GATED_FINE = 0x100
 FD_ROUNDING = {"nearest": 0, "unbiased": 1}
 FD_KERNEL_PRODUCT, FD_KERNEL_ROWSUM = 0, 1
 
@@ -752,7 +753,7 @@ def fd_layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[to
     return LayerNormGrads(dX, dgamma, dbeta)
 
 
-def _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act) -> GatedBlock:
+def _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act, fine=False) -> GatedBlock:
     if X.dim() != 2 or Wg.dim() != 2 or Wd.dim() != 2:
         raise ValueError("X, Wg, Wu and Wd must be matrices")
     if act not in FD_ACT:
@@ -767,7 +768,7 @@ def _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act) -> GatedBlock:
     if _net_matrix(Wu, F, D, t, dev, "Wu") != ldwi:
         raise ValueError("Wg and Wu must have the same leading dimension")
     ldwd = _net_matrix(Wd, O, F, t, dev, "Wd")
-    return GatedBlock(N, D, F, O, code, FD_ACT[act], X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(),
+    return GatedBlock(N, D, F, O, code, FD_ACT[act] | (FD_GATED_FINE if fine else 0), X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(),
                       Wd.data_ptr(), _net_vector(bg, F, t, dev, "bg"), _net_vector(bu, F, t, dev, "bu"),
                       _net_vector(bd, O, t, dev, "bd"), ldx, ldwi, ldwd)
 
@@ -776,13 +777,14 @@ def fd_gated_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: to
                      bg: Optional[torch.Tensor] = None, bu: Optional[torch.Tensor] = None,
                      bd: Optional[torch.Tensor] = None, R: Optional[torch.Tensor] = None,
                      act: str = "silu", save: bool = False, Y: Optional[torch.Tensor] = None,
-                     ws: Optional[torch.Tensor] = None
+                     ws: Optional[torch.Tensor] = None, fine: bool = False
                      ) -> "tuple[torch.Tensor, Optional[torch.Tensor]]":
     """(Y, saved): Y = (act(X Wg^T + bg) * (X Wu^T + bu)) Wd^T + bd [+ R];
     saved (with save) is what fd_gated_backward takes to spare computing the
-    inner activations again."""
+    inner activations again.  fine: bfloat16 inner values are not rounded to one
+    bfloat16, at any size.  The results have no autograd history."""
     lib = load()
-    b = _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act)
+    b = _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act, fine)
     dev = X.get_device()
     if Y is None:
         Y = X.new_empty((b.N, b.O))
@@ -816,11 +818,11 @@ def fd_gated_backward(dY: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: t
                       bu: Optional[torch.Tensor] = None, bd: Optional[torch.Tensor] = None,
                       act: str = "silu", saved: Optional[torch.Tensor] = None,
                       want_dx: bool = True, grads: Optional[GatedGrads] = None,
-                      ws: Optional[torch.Tensor] = None) -> GatedGrads:
+                      ws: Optional[torch.Tensor] = None, fine: bool = False) -> GatedGrads:
     """Gradients of fd_gated_forward (R's is dY itself), into `grads` where
-    given; a bias has one where it was given."""
+    given; a bias has one where it was given.  fine: as in the forward pass, by itself."""
     lib = load()
-    b = _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act)
+    b = _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act, fine)
     dev, t = X.get_device(), X.dtype
     lddy = _net_matrix(dY, b.N, b.O, t, dev, "dY")
     if grads is None:

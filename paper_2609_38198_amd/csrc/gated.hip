@@ -430,11 +430,15 @@ void shapes_grad(const fd_gated_block& b, Shape (&s)[GROUP_GEMMS]) {
 // are not what takes the time, what was rounded off is a second plane: 19 -> 19.4 us at
 // 2 x 32 -> 32 -> 28 (forward and backward), 29 -> 30 at 64 x 128 -> 256 -> 128,
 // 31 -> 33 at 256 x 128 -> 512 -> 128; but 42 -> 52 at 1,024 x 256 -> 512 -> 256, and 147
-// -> 232 at 5,003 x 509 -> 1365 -> 509, which keep one.
+// -> 232 at 5,003 x 509 -> 1365 -> 509, which keep one unless the caller asks for two (4.6 ->
+// 14.8 ms at 16,384 x 2048 -> 8192 -> 2048: two planes take the smallest tiles alone).
 constexpr double FINE_WORK = double(1 << 25);
 bool fine(const fd_gated_block& b) {
-  return b.type == FD_BF16 && double(b.N) * double(b.F) * double(std::max(b.D, b.O)) <= FINE_WORK;
+  if (b.type != FD_BF16) return false;
+  return (b.act & FD_GATED_FINE) != 0 ||
+         double(b.N) * double(b.F) * double(std::max(b.D, b.O)) <= FINE_WORK;
 }
+int activation_of(const fd_gated_block& b) { return b.act & ~FD_GATED_FINE; }
 
 template <class T>
 Work carve_work_t(Arena& a, const fd_gated_block& b, int backward) {
@@ -541,7 +545,7 @@ void run_gate(const fd_gated_block& b, const Work& w, const Matrix& x, const Mat
   p.Fp = f_padded(b.F);
   p.H = h ? w.h : nullptr;
   p.hplane = b.N * p.Fp;
-  const auto run = b.act == FD_ACT_SILU ? launch_inner<false, GATE, T, FD_ACT_SILU, HP>
+  const auto run = activation_of(b) == FD_ACT_SILU ? launch_inner<false, GATE, T, FD_ACT_SILU, HP>
                                         : launch_inner<false, GATE, T, FD_ACT_GELU, HP>;
   run(w.gate_config, w.gate, w.part, p, st);
 }
@@ -557,8 +561,8 @@ void check_block(const fd_gated_block* bp) {
 }
 
 void check_arrays(const fd_gated_block& b) {
-  FD_REQUIRE(b.act == FD_ACT_SILU || b.act == FD_ACT_GELU, FD_ERR_INVALID_ARG,
-             "unknown activation");
+  FD_REQUIRE(activation_of(b) == FD_ACT_SILU || activation_of(b) == FD_ACT_GELU,
+             FD_ERR_INVALID_ARG, "unknown activation");
   FD_REQUIRE(b.Wg != nullptr && b.Wu != nullptr && b.Wd != nullptr, FD_ERR_INVALID_ARG,
              "a weight is NULL");
   FD_REQUIRE(b.N == 0 || b.X != nullptr, FD_ERR_INVALID_ARG, "X is NULL");
@@ -611,7 +615,7 @@ void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void*
     SkinnyArgs p{b.X,  b.Wg,    b.Wu, b.ldx, b.ldwi, b.N, b.F, b.D,
                  b.bg, b.bu, nullptr,     0,    w.h,  Fp,   0, plane};
     constexpr int SP = sizeof(T) == 4 ? 1 : HP;
-    if (b.act == FD_ACT_SILU) launch_skinny<T, SP, true, FD_ACT_SILU>(p, st);
+    if (activation_of(b) == FD_ACT_SILU) launch_skinny<T, SP, true, FD_ACT_SILU>(p, st);
     else launch_skinny<T, SP, true, FD_ACT_GELU>(p, st);
     p = SkinnyArgs{w.h,  b.Wd,    nullptr, Fp,  b.ldwd, b.N, b.O,   b.F,
                    b.bd, nullptr, R,       ldr, Y,      ldy, plane, 0};
@@ -621,6 +625,7 @@ void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void*
   if (b.D <= NARROW && b.O <= NARROW) {
     NarrowArgs p{b,      R,    ldr, Y, ldy, saved, f_padded(b.F), narrow_parts(b.N, b.F),
                  w.part, round_up(b.O, 4)};
+    p.b.act = activation_of(b);
     run_narrow(p, HP, st);
     if (p.parts == 1) return;
     AfterJobs after;
@@ -721,7 +726,7 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
     p.dGU = w.dgu;
     p.gplane = b.N * 2 * Fp;
     p.colsum = g.dbg != nullptr || g.dbu != nullptr ? w.colsum : nullptr;
-    const auto run = b.act == FD_ACT_SILU ? launch_inner<true, GRAD, T, FD_ACT_SILU, HP>
+    const auto run = activation_of(b) == FD_ACT_SILU ? launch_inner<true, GRAD, T, FD_ACT_SILU, HP>
                                           : launch_inner<true, GRAD, T, FD_ACT_GELU, HP>;
     run(w.grad_config, w.grad, w.part, p, st);
     const int64_t sum_rows = w.grad.splits > 1

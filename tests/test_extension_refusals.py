@@ -135,3 +135,15 @@ def test_layer_norm_gradients_types():
     for kw in (dict(gamma=half), dict(gamma=None, dbeta=half), dict(gamma=None, wdtype=torch.float64)):
         with pytest.raises(TypeError):
             fd.fd_layer_norm_backward(x, x, stats=ms, **kw)
+
+
+def test_fine_flag_and_unknown_activations():
+    lib = fd.load()
+    kw = dict(N=5003, D=509, F=1365, O=509, type=1, X=256, Wg=256, Wu=256, Wd=256, ldx=509, ldwi=509,
+              ldwd=1365)
+    coarse, fine = fd.GatedBlock(act=1, **kw), fd.GatedBlock(act=1 | fd.FD_GATED_FINE, **kw)
+    for backward in (0, 1, 2):
+        assert lib.fd_gated_workspace_size(fine, backward) > lib.fd_gated_workspace_size(coarse, backward) > 0
+    for act in (2, fd.FD_GATED_FINE | 2, 0x200, -1):
+        b = fd.GatedBlock(act=act, **kw)
+        assert lib.fd_gated_forward(b, None, 0, 256, 509, None, 0, 256, 1 << 40, None) == 1, act

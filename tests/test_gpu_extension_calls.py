@@ -55,3 +55,28 @@ def test_one_row_has_no_leading_dimension(dtype):
     for name in ("dX", "dWg", "dWu", "dWd"):
         assert torch.equal(getattr(g, name), getattr(g0, name)), name
     assert to_np(g.dWg).any()
+
+
+# What is off is the rounding of the float64 values itself, and 2^-15 of the kept G and U: the
+# bound of small problems, at sizes that would round H, dG and dU to one bfloat16 without it.
+@pytest.mark.parametrize("n, d, f, o, act", [(5003, 509, 365, 260, "silu"), (1200, 96, 640, 520, "gelu"),
+                                             (70000, 40, 128, 48, "silu")])
+def test_gated_fine_is_rounded_once_at_any_size(n, d, f, o, act):
+    t, a = gated_inputs(n, d, f, o, BF16, True, n + o)
+    case(f"gated, fine {(n, d, f, o)} {act}")
+    w = [t[k] for k in WEIGHTS]
+    inner = [a[k] for k in WEIGHTS[:6]]
+    want = dict(ox.gated_backward(a["dY"], *inner, act), Y=ox.gated(*inner, a["bd"], act=act)[0])
+
+    def ratio(got, name):
+        once = torch.from_numpy(want[name]).to(BF16).double().numpy()
+        return np.linalg.norm(to_np(got) - want[name]) / np.linalg.norm(once - want[name])
+
+    for save in (False, True):
+        Y, saved = fd.fd_gated_forward(*w, act=act, save=save, fine=True)
+        g = fd.fd_gated_backward(t["dY"], *w, act=act, saved=saved, fine=True)
+        off = {k: ratio(Y if k == "Y" else getattr(g, k), k) for k in ("Y", "dX", "dWg", "dWu", "dWd")}
+        assert max(off.values()) <= 1.1, off
+    # float32 takes the flag and does as before
+    x = [None if v is None else v.float() for v in w]
+    assert torch.equal(fd.fd_gated_forward(*x, act=act)[0], fd.fd_gated_forward(*x, act=act, fine=True)[0])
