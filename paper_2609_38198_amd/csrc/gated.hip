@@ -179,36 +179,6 @@ __global__ __launch_bounds__(GROUP) void clear_kernel(T* p, int64_t rows, int64_
 
 // ---------------------------------------------------------------- products
 
-// Tiles of C and what they cost on an MI355X (us, measured at 256 to 16384 rows
-// x 512 to 2048 -> 2048 to 8192 and ragged ones): a k tile as a CU's share among as many workgroups
-// as fit (operands by rows; by columns, where small tiles read LDS in twice as many
-// instructions), a k tile of a workgroup alone, and the rest of a workgroup by
-// epilogue.
-struct TileCost {
-  int bm, bn, per_cu;
-  double k[2], alone, rest[3];  // rest: STORE, GATE, GRAD
-};
-enum { BIG = 0, MID = 1, SMALL = 2, CONFIGS = 3 };
-constexpr int64_t CUS = 256;
-
-// bfloat16: 256 x 256 by eight waves of 128 x 64, whose LDS reads (96 bytes a
-// clock at the matrix unit's full rate) stay below the CU's 128 (four waves of 128 x 128
-// read 64, but nothing hides their waits: 5.39 ms against 4.68 for the whole of 16,384 x
-// 2048 -> 8192); 128 x 128 by four waves of 64 x 64, which take all of them (6.09 ms); 64 x
-// 64 by four waves of 32 x 32.  With all later steps: 4.52 ms, 1,090 TFLOP/s.
-// float32 (three planes): 256 x 128 and 128 x 128 by waves of 64 x 64 (64
-// bytes a clock), 64 x 64.  8,192 x 1024 -> 4096: 3.3 ms, 1,120 TFLOP/s of bfloat16 products.
-template <class T>
-const TileCost* tile_costs() {
-  static const TileCost wide[CONFIGS] = {{256, 256, 1, {1.9, 1.9}, 1.65, {5, 14, 28}},
-                                         {128, 128, 2, {0.56, 0.56}, 0.85, {4, 8, 14}},
-                                         {64, 64, 5, {0.20, 0.30}, 0.80, {3, 6, 8}}};
-  static const TileCost three[CONFIGS] = {{256, 128, 1, {2.7, 2.7}, 2.5, {6, 17, 40}},
-                                          {128, 128, 1, {1.65, 1.65}, 1.5, {5, 12, 22}},
-                                          {64, 64, 3, {0.50, 0.50}, 0.74, {3, 6, 9}}};
-  return sizeof(T) == 4 ? three : wide;
-}
-
 template <int C, int EPI, class T>
 struct Config;  // BM, BN, WM, WN
 template <int EPI, class T>
@@ -224,67 +194,6 @@ template <int EPI, class T>
 struct Config<SMALL, EPI, T> {
   static constexpr int bm = 64, bn = 64, wm = 2, wn = EPI == GATE ? 1 : 2;
 };
-
-// Extents and k tiles of a product, and how it is to run.
-struct Shape {
-  int64_t M = 0, N = 0, ktiles = 0;
-  int splits = 1;
-  size_t part() const { return splits == 1 ? 0 : size_t(splits) * size_t(M) * size_t(round_up(N, 4)); }
-};
-
-// The tile (the smallest with `fine`), and the parts of each product's k, of a launch of
-// `count` products: the least of an estimate that counts whole rounds of a
-// workgroup a CU, the longest workgroup, and the traffic of the parts' sums.
-template <class T>
-int plan(Shape* s, int count, bool fine, int epilogue, bool columns) {
-  const TileCost* costs = tile_costs<T>();
-  double best = 1e30;
-  int config = SMALL;
-  int parts[GROUP_GEMMS] = {1, 1, 1};
-  for (int c = fine ? SMALL : BIG; c < CONFIGS; ++c) {
-    const TileCost& t = costs[c];
-    const double rest = t.rest[epilogue];
-    double tiles[GROUP_GEMMS], k[GROUP_GEMMS], mn[GROUP_GEMMS];
-    for (int i = 0; i < count; ++i) {
-      tiles[i] = double(ceil_div(s[i].M, t.bm) * ceil_div(s[i].N, t.bn));
-      k[i] = double(s[i].ktiles);
-      mn[i] = double(s[i].M) * double(s[i].N);
-    }
-    const bool may = epilogue == STORE || c != BIG;
-    for (int cap = may ? 4 : 1024; cap <= 1024; cap *= 2) {
-      // of the products longer than the cap, those in the mask are split
-      for (int mask = 0; mask < (may ? 1 << count : 1); ++mask) {
-        double groups = 0, work = 0, longest = 0, sums = 0;
-        int n[GROUP_GEMMS];
-        bool fresh = true;
-        for (int i = 0; i < count; ++i) {
-          n[i] = 1;
-          if (mask >> i & 1) {
-            if (s[i].ktiles <= cap) fresh = false;  // the same as without it
-            n[i] = int(std::max<int64_t>(1, ceil_div(s[i].ktiles, int64_t(cap))));
-          }
-          const double each = k[i] / n[i];
-          groups += tiles[i] * n[i];
-          work += tiles[i] * n[i] * (each * t.k[columns] + rest / t.per_cu);
-          longest = std::max(longest, each * t.alone + rest);
-          if (n[i] > 1) sums += mn[i] * 4.0 * (2 * n[i] + 1) / 4.0e6;  // 4 TB/s
-        }
-        if (!fresh) continue;
-        const double rounds = groups / double(CUS);
-        const double full = work / double(CUS) * std::ceil(rounds) / std::max(rounds, 1e-9);
-        const double time = std::max(full, longest) +
-                            (sums > 0 ? sums + (epilogue == STORE ? 4.0 : 8.0) : 0.0);
-        if (time < best) {
-          best = time;
-          config = c;
-          for (int i = 0; i < count; ++i) parts[i] = n[i];
-        }
-      }
-    }
-  }
-  for (int i = 0; i < count; ++i) s[i].splits = parts[i];
-  return config;
-}
 
 template <class K>
 void allow_lds(K kernel, size_t bytes) {
@@ -386,15 +295,8 @@ struct Work {
   float *part = nullptr, *colsum = nullptr, *dysum = nullptr;
   char* saved = nullptr;
   PackJobs jobs;
-  // the forward pass's Y, or the backward pass's dX, [dWg; dWu], dWd
-  Shape shapes[GROUP_GEMMS];
-  int config = SMALL;
-  // G and U; dH
-  Shape gate, grad;
-  int gate_config = SMALL, grad_config = SMALL;
+  GatedPlan plan;
 };
-
-int64_t f_padded(int64_t F) { return round_up(F, F_PAD); }
 
 template <class T>
 size_t packed(int64_t rows, int64_t cols) {
@@ -409,19 +311,6 @@ size_t saved_bytes_t(int64_t N, int64_t F) {
 }
 size_t saved_bytes(const fd_gated_block& b) {
   return b.type == FD_F32 ? saved_bytes_t<float>(b.N, b.F) : saved_bytes_t<bf16>(b.N, b.F);
-}
-
-// Shapes of the products: Y; and dX, [dWg; dWu], dWd.
-template <class T>
-Shape shape_y(const fd_gated_block& b) {
-  return Shape{b.N, b.O, f_padded(b.F) / k_tile<T>};
-}
-template <class T>
-void shapes_grad(const fd_gated_block& b, Shape (&s)[GROUP_GEMMS]) {
-  const int64_t Fp = f_padded(b.F), nt = ceil_div(b.N, k_tile<T>);
-  s[0] = Shape{b.N, b.D, 2 * Fp / k_tile<T>};
-  s[1] = Shape{2 * Fp, b.D, nt};
-  s[2] = Shape{b.O, b.F, nt};
 }
 
 // Planes of H, dG and dU.  One bfloat16 plane rounds them once more than 32-bit
@@ -452,16 +341,11 @@ Work carve_work_t(Arena& a, const fd_gated_block& b, int backward) {
   const bool two = fine(b);
   const int inner = two ? 2 : planes_of<T>;
   w.h = a.take<bf16>(size_t(b.N) * Fp * inner);  // (few rows of float32: as they are)
-  size_t part = 0;
-  if (backward != 1) {
-    w.gate = Shape{b.N, 2 * b.F, ceil_div(b.D, k_tile<T>)};
-    w.gate_config = plan<T>(&w.gate, 1, two, GATE, false);
-    if (w.gate.splits > 1) part = size_t(w.gate.splits) * blocks * 2048;
-  }
+  w.plan = plan_gated(b.N, b.D, b.F, b.O, sizeof(T) == 4, two, backward);
+  const GatedPlan& p = w.plan;
+  size_t part = p.gate.splits > 1 ? size_t(p.gate.splits) * blocks * 2048 : 0;
   if (backward == 0) {
-    w.shapes[0] = shape_y<T>(b);
-    w.config = plan<T>(w.shapes, 1, two, STORE, false);
-    part = std::max(part, w.shapes[0].part());
+    part = std::max(part, p.out[0].part());
     if (b.D <= NARROW && b.O <= NARROW)
       part = std::max(part, size_t(narrow_parts(b.N, b.F)) * size_t(b.N) * size_t(round_up(b.O, 4)));
   } else {
@@ -471,13 +355,9 @@ Work carve_work_t(Arena& a, const fd_gated_block& b, int backward) {
     // rows have two, of 256 rows at most four
     w.colsum = a.take<float>(size_t(2 * ceil_div(b.N, 64) + 2) * 2 * Fp);
     w.dysum = a.take<float>(size_t(SUM_PARTS) * size_t(b.O));
-    shapes_grad<T>(b, w.shapes);
-    w.config = plan<T>(w.shapes, GROUP_GEMMS, two, STORE, true);
     size_t sum = 0;
-    for (const Shape& s : w.shapes) sum += s.part();
-    w.grad = Shape{b.N, b.F, ceil_div(b.O, k_tile<T>)};
-    w.grad_config = plan<T>(&w.grad, 1, two, GRAD, true);
-    part = std::max({part, sum, w.grad.splits > 1 ? size_t(w.grad.splits) * blocks * 1024 : 0});
+    for (const Shape& s : p.out) sum += s.part();
+    part = std::max({part, sum, p.grad.splits > 1 ? size_t(p.grad.splits) * blocks * 1024 : 0});
     if (backward == 2) w.saved = a.take<char>(saved_bytes(b));
   }
   w.part = a.take<float>(part);
@@ -547,7 +427,7 @@ void run_gate(const fd_gated_block& b, const Work& w, const Matrix& x, const Mat
   p.hplane = b.N * p.Fp;
   const auto run = activation_of(b) == FD_ACT_SILU ? launch_inner<false, GATE, T, FD_ACT_SILU, HP>
                                         : launch_inner<false, GATE, T, FD_ACT_GELU, HP>;
-  run(w.gate_config, w.gate, w.part, p, st);
+  run(w.plan.gate_config, w.plan.gate, w.part, p, st);
 }
 
 void check_block(const fd_gated_block* bp) {
@@ -610,7 +490,8 @@ template <class T, int HP>
 void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void* Y, int64_t ldy,
              char* saved, hipStream_t st) {
   const int t = b.type;
-  if (b.N <= skinny_rows<T> && saved == nullptr) {
+  const Way way = forward_way(b.N, b.D, b.O, sizeof(T) == 4, saved != nullptr);
+  if (way == FEW_ROWS) {
     const int64_t Fp = f_padded(b.F), plane = b.N * Fp;
     SkinnyArgs p{b.X,  b.Wg,    b.Wu, b.ldx, b.ldwi, b.N, b.F, b.D,
                  b.bg, b.bu, nullptr,     0,    w.h,  Fp,   0, plane};
@@ -622,7 +503,7 @@ void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void*
     launch_skinny<T, SP, false, 0>(p, st);
     return;
   }
-  if (b.D <= NARROW && b.O <= NARROW) {
+  if (way == NARROW_WAY) {
     NarrowArgs p{b,      R,    ldr, Y, ldy, saved, f_padded(b.F), narrow_parts(b.N, b.F),
                  w.part, round_up(b.O, 4)};
     p.b.act = activation_of(b);
@@ -657,8 +538,8 @@ void forward(const fd_gated_block& b, Work& w, const void* R, int64_t ldr, void*
   p.ldr = ldr;
   AfterJobs after;
   float* room = w.part;
-  set_parts(p, w.shapes[0], room, after);
-  launch<false, false, STORE, T, 0, HP>(w.config, p, st);
+  set_parts(p, w.plan.out[0], room, after);
+  launch<false, false, STORE, T, 0, HP>(w.plan.config, p, st);
   run_after<T>(after, st);
 }
 
@@ -728,10 +609,10 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
     p.colsum = g.dbg != nullptr || g.dbu != nullptr ? w.colsum : nullptr;
     const auto run = activation_of(b) == FD_ACT_SILU ? launch_inner<true, GRAD, T, FD_ACT_SILU, HP>
                                           : launch_inner<true, GRAD, T, FD_ACT_GELU, HP>;
-    run(w.grad_config, w.grad, w.part, p, st);
-    const int64_t sum_rows = w.grad.splits > 1
+    run(w.plan.grad_config, w.plan.grad, w.part, p, st);
+    const int64_t sum_rows = w.plan.grad.splits > 1
                                  ? ceil_div(b.N, 32)
-                                 : p.tiles_m * grad_wave_rows<T>(w.grad_config);
+                                 : p.tiles_m * grad_wave_rows<T>(w.plan.grad_config);
 
     const Matrix h{w.h, Fp, b.N, Fp, b.N * Fp}, dgu{w.dgu, 2 * Fp, b.N, 2 * Fp, b.N * 2 * Fp};
     Shape shapes[GROUP_GEMMS];
@@ -747,7 +628,7 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
       q.out[0] = g.dX;
       q.ldo = g.lddx;
       q.half = q.rows = b.N;
-      shapes[group.count++] = w.shapes[0];
+      shapes[group.count++] = w.plan.out[0];
     }
     if (inner_weights) {  // [dG dU]^T X
       GemmArgs& q = group.g[group.count];
@@ -761,7 +642,7 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
       q.half = Fp;
       q.rows = b.F;
       group.acol[group.count] = true;
-      shapes[group.count++] = w.shapes[1];
+      shapes[group.count++] = w.plan.out[1];
     }
     if (g.dWd != nullptr) {  // dY^T H
       GemmArgs& q = group.g[group.count];
@@ -773,7 +654,7 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
       q.ldo = g.lddwd;
       q.half = q.rows = b.O;
       group.acol[group.count] = group.inner[group.count] = true;
-      shapes[group.count++] = w.shapes[2];
+      shapes[group.count++] = w.plan.out[2];
     }
     if (group.count > 0) {
       float* room = w.part;
@@ -784,8 +665,8 @@ void backward(const fd_gated_block& b, Work& w, const void* dY, int64_t lddy, ch
       }
       auto run = launch_group<SMALL, T, HP>;
       if constexpr (HP == planes_of<T>) {
-        if (w.config == BIG) run = launch_group<BIG, T, HP>;
-        if (w.config == MID) run = launch_group<MID, T, HP>;
+        if (w.plan.config == BIG) run = launch_group<BIG, T, HP>;
+        if (w.plan.config == MID) run = launch_group<MID, T, HP>;
       }
       run(group, st);
     }

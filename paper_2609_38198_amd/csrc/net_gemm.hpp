@@ -10,16 +10,16 @@
 #pragma once
 
 #include "net_common.hpp"
+#include "net_plans.hpp"
 
 namespace fd {
 namespace net {
 
-constexpr int F_PAD = 64;        // inner widths are padded to whole k tiles
 constexpr int MAX_SEGS = 2;      // matrices contracted one after the other
 template <class T>
 constexpr int planes_of = sizeof(T) == 4 ? 3 : 1;
 template <class T>
-constexpr int k_tile = sizeof(T) == 4 ? 32 : 64;  // k of an LDS tile
+constexpr int k_tile = k_extent(sizeof(T) == 4);  // k of an LDS tile
 constexpr int64_t MAX_LD = int64_t(1) << 22;      // a tile's byte offsets stay below 2^31
 
 // Sixteen bytes of zeros that lanes past the end of k read.
@@ -235,13 +235,6 @@ __device__ __forceinline__ Act activate(float g) {
   }
   return a;
 }
-
-// What a product does with its accumulators.
-enum Epilogue {
-  STORE = 0,  // C (+ bias + R) in T, or a split's float32 partial sums
-  GATE = 1,   // B is [Wg; Wu]: H = act(G) U as planes, G and U kept where wanted
-  GRAD = 2    // C is dH: dG, dU, H as planes from the kept G and U, column sums
-};
 
 struct GemmArgs {
   Operand a, b;
@@ -800,7 +793,6 @@ __global__ __launch_bounds__(WM * WN * WAVE) void gemm_kernel(GemmArgs p) {
 
 // The backward pass's last products, which do not depend on each other, in one
 // launch: the workgroups of one fill what another leaves idle.
-constexpr int GROUP_GEMMS = 3;
 struct GemmGroup {
   GemmArgs g[GROUP_GEMMS];
   bool acol[GROUP_GEMMS];          // a in column order (b always is)

@@ -5,11 +5,11 @@
 #include <algorithm>
 
 #include "net_common.hpp"
+#include "net_plans.hpp"
 
 namespace fd {
 namespace net {
 
-constexpr int64_t NARROW = 64;
 constexpr int64_t NARROW_ROWS = 128;  // of a workgroup
 // Parts of F until every CU has a workgroup, two steps each at least.
 inline int narrow_parts(int64_t N, int64_t F) {

@@ -8,11 +8,6 @@
 namespace fd {
 namespace net {
 
-// Up to so many rows: 16 rows more are another pass of the matrix unit and of
-// the rows' own loads, and the tiled product overtakes (2048 -> 8192 -> 2048: bfloat16 42 us
-// at 32 rows, 61 at 64 against the tiles' 39; float32 132 at 64 against 210).
-template <class T>
-constexpr int64_t skinny_rows = sizeof(T) == 4 ? 64 : 32;
 constexpr int SKINNY_WAVES = 16;  // waves x 16-row blocks of a workgroup at most
 
 struct SkinnyArgs {
