@@ -514,7 +514,8 @@ void fd_adamw_default_opts(fd_adamw_opts* opts);
  * element that is not finite is kept as NaN and leaves its neighbours alone.
  * Clear m, v and the scales before the first step.
  * The pointers travel with the launches (the tensors of one call share a few):
- * the array may go once the call returns. */
+ * the array may go once the call returns.  Under graph capture the options do too, the step's
+ * number among them: a replay is that step again. */
 fd_status fd_adamw_step(const fd_adamw_tensor* tensors, int64_t count, const fd_adamw_opts* opts,
                         void* stream);
 
