@@ -677,7 +677,8 @@ def fd_layer_norm(X: torch.Tensor, gamma: Optional[torch.Tensor] = None,
                   beta: Optional[torch.Tensor] = None, eps: float = 1e-5,
                   Y: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None
                   ) -> "tuple[torch.Tensor, torch.Tensor]":
-    """(Y, stats): (x - mean) rstd gamma + beta of each row of X, and its (mean, rstd)."""
+    """(Y, stats): (x - mean) rstd gamma + beta of each row of X, and its (mean, rstd).
+    The results have no autograd history (nor have those of the calls below)."""
     lib = load()
     if X.dim() != 2:
         raise ValueError("X must be N x D")
@@ -782,7 +783,7 @@ def fd_gated_forward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: to
     """(Y, saved): Y = (act(X Wg^T + bg) * (X Wu^T + bu)) Wd^T + bd [+ R];
     saved (with save) is what fd_gated_backward takes to spare computing the
     inner activations again.  fine: bfloat16 inner values are not rounded to one
-    bfloat16, at any size.  The results have no autograd history."""
+    bfloat16, at any size."""
     lib = load()
     b = _gated_block(X, Wg, Wu, Wd, bg, bu, bd, act, fine)
     dev = X.get_device()
@@ -888,9 +889,9 @@ class AdamwPlan:
 def fd_adamw_plan(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
                   state: AdamwState, copies: Optional[Sequence[torch.Tensor]] = None,
                   decay: Optional[Sequence[float]] = None) -> AdamwPlan:
-    """Tensors that fd_adamw_step updates: float32 params from float32 or
-    bfloat16 grads, optionally bfloat16 copies of the params, and a multiplier of
-    the weight decay for each (default 1)."""
+    """Tensors that fd_adamw_step updates, by their addresses (gradients that moved take a
+    new plan, 2.5 us a tensor): float32 params from float32 or bfloat16 grads, optionally
+    bfloat16 copies of the params, and a multiplier of the weight decay for each (default 1)."""
     n = len(params)
     bits = 32 if state.m_scale is None else 8
     lists = [params, grads, state.m, state.v]

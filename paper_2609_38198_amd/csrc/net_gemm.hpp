@@ -4,8 +4,9 @@
 // Operands come in two orders: "rows" (k contiguous: p[m ld + k]) and "columns"
 // (m contiguous: p[k ld + m]), so that no operand is ever transposed in memory:
 // column tiles are transposed by the LDS read itself.  float32 operands enter
-// as three bfloat16 planes (x = x0 + x1 + x2 to 24 bits); the six plane pairs whose
-// product reaches 2^-24 of x y are multiplied from one tile of all planes.  Six
+// as three bfloat16 planes (x = x0 + x1 + x2 to 24 bits; x1 is below 2^-7 of x, x2 below
+// 2^-16); the six largest of the nine plane pairs are multiplied from one tile of all
+// planes.  The next two, x1 y2 and x2 y1, are at most 2^-23 of x y each.  Six
 // products at the bfloat16 rate are 1.5 times the float32 unit's peak.
 #pragma once
 
@@ -383,7 +384,7 @@ __device__ __forceinline__ void write_planes(bf16* p, int64_t plane, const float
 }
 
 // The plane pairs of a product that are worth their time, smallest first: all
-// with one plane on a side, of 3 x 3 those that reach 2^-24.
+// with one plane on a side, of 3 x 3 the six largest.
 template <int PLA, int PLB>
 struct Pairs {
   static constexpr bool SIX = PLA == 3;

@@ -140,8 +140,8 @@ GATED_SHAPES = [(1, 1, 1, 1), (1, 4, 16, 4), (1, 1024, 512, 256), (2, 30, 97, 64
                 (16, 257, 300, 129), (17, 64, 64, 64), (31, 33, 65, 31), (64, 512, 1024, 512),
                 (127, 130, 191, 66), (129, 128, 128, 128), (200, 8, 24, 16), (257, 509, 333, 509),
                 (1000, 30, 512, 64), (2049, 96, 160, 72), (3000, 16, 40, 8),
-                # every tile of each product: many rows, wide inner, wide outer sides
-                # few tiles and long sums over D and O
+                # many rows, wide inner, wide outer sides, few tiles and long sums over D and O (the
+                # tiles that these do not take: test_gpu_extension_tiles.py)
                 (70, 2000, 90, 1500), (336, 1696, 372, 700),
                 (33000, 7, 70, 33), (501, 33, 31, 64), (4100, 24, 2100, 16), (4104, 4100, 40, 4098), (700, 40, 4099, 2050)]
 
@@ -248,8 +248,8 @@ def test_gated_single_gradients(dtype):
 
 
 # Small problems round to bfloat16 nowhere but at the end: what is off is the rounding of the
-# float64 values itself, and an eighth of it from the kept 11-bit G and U (by
-# derivatives of up to two or three: 1.07 in all); H, dG and dU once rounded would give 1.4.
+# float64 values itself, and 2^-15 of the kept G and U (1.1 leaves room for an eighth of the
+# rounding, by derivatives of up to two or three); H, dG and dU once rounded would give 1.4.
 @pytest.mark.parametrize("n, d, f, o", [(1, 600, 900, 700), (30, 96, 128, 80), (24, 128, 333, 96),
                                         (100, 30, 97, 64), (150, 64, 640, 40), (70, 200, 72, 90),
                                         (257, 129, 250, 101), (64, 700, 64, 500)])
